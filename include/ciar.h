@@ -361,6 +361,159 @@ int ciar_interhead_logits_timed(const void* hidden, const void* weight, const fl
                                 int64_t N, const ciar_params* params, float* centre, float* radius,
                                 void* hip_stream, void* start_event, void* stop_event);
 
+/* ---- The verification step around the accept test: paged cache, attention over it, the logits' adjustments ----
+ *
+ * Before ciar_verify can test a window, the verifier runs on the drafted tokens: their places in a paged cache of keys
+ * and values are planned (ciar_cache_plan), queries and keys are turned by their positions and keys and values laid into
+ * the pages (ciar_rotary), every new token attends to what its request has in the cache (ciar_paged_attention), and the
+ * logits take their penalties, biases and grammar masks (ciar_adjust_logits).  All four enqueue on `hip_stream`, allocate
+ * nothing and read nothing back: the counts the host does not know (accepted lengths) stay on the device.
+ *
+ * Layout of a cache of `cache_pages` pages of `page_size` tokens (a multiple of 16), bfloat16, an atom of 16 tokens of one
+ * head at a time, each contiguous:
+ *   keys   [cache_pages, kv_heads, page_size / 16, head_dim / 8, 16, 8]   token t of the atom, dimension d: [d / 8, t, d % 8]
+ *   values [cache_pages, kv_heads, page_size / 16, 2, head_dim, 8]        token t of the atom, dimension d: [t / 8, d, t % 8]
+ * (sixteen consecutive bytes are what a lane hands to a matrix instruction, so tiles are used as they lie in memory).
+ * Slot s is token s % page_size of page s / page_size.
+ */
+
+/*
+ * Plans one step: R requests, request r holding lengths[r] + kept[r] tokens in the cache (kept: what the last window's
+ * verification has accepted, at most what was drafted; NULL = 0) in the held[r] pages that open its row of `table`, is
+ * about to add new_tokens[r] tokens.
+ *   pages[r]   = ceil((lengths[r] + kept[r] + new_tokens[r]) / page_size)
+ *   granted[r] = request r's new tokens end within the first T of the step's and its pages within table_width, and the free
+ *                pages suffice for it and all requests before it (requests that need no page are granted then too)
+ * Pages that a granted request lacks are taken from the ring of free pages, first come first served, and written behind
+ * table[r][held[r] - 1]; pages that it holds beyond pages[r] (a rejected tail) go back to the ring's tail (their table
+ * entries stay, unused).  The ring: `ring` [ring_pages], entry i of its life at ring[i % ring_pages], ring_state = {taken so
+ * far, put back so far}; free pages = ring_state[1] - ring_state[0].  `ring` and `table` are updated in place, nothing else
+ * is, and outputs must not overlap inputs (several workgroups read the inputs).
+ *   out_lengths [R]  lengths + kept                       kv_len [R]   out_lengths + new_tokens, 0 if not granted
+ *   cu_new [R + 1]   first new token of each request (running sum, at most T)
+ *   out_held [R]     pages held now                       granted [R]  uint8
+ *   out_ring_state [2]
+ *   slots, positions, requests [T]   cache slot (-1: not granted, or no token), position in the request (0: no token) and
+ *                                    request (-1: no token) of each new token
+ * Preconditions: 0 <= lengths, kept, new_tokens; 0 <= held <= table_width; no page twice in the ring and the tables.  What
+ * breaks them gives unspecified numbers, never a fault.  table_width * page_size and ring_pages * page_size <= 2^31 - 1.
+ */
+int ciar_cache_plan(const int32_t* lengths, const int32_t* kept, const int32_t* new_tokens, const int32_t* held, int64_t R,
+                    int32_t* ring, int64_t ring_pages, const int64_t* ring_state, int32_t* table, int32_t table_width,
+                    int64_t table_stride, int32_t page_size, int64_t T,
+                    int32_t* out_lengths, int32_t* kv_len, int32_t* cu_new, int32_t* out_held, uint8_t* granted,
+                    int64_t* out_ring_state, int32_t* slots, int32_t* positions, int32_t* requests, void* hip_stream);
+
+typedef struct ciar_rotary_params {
+    uint32_t struct_size;     /* sizeof(ciar_rotary_params); checked                                        */
+    int32_t  dtype;           /* ciar_dtype of q, k, v; CIAR_BF16 where a cache is given                    */
+    int32_t  q_heads, kv_heads;
+    int32_t  head_dim;        /* D; a multiple of 8 where a cache is given                                  */
+    int32_t  rotary_dim;      /* the first n dimensions of a head are turned; even, 2 <= n <= D             */
+    int32_t  interleaved;     /* 0: pair p is (p, p + n / 2), 1: pair p is (2 p, 2 p + 1)                   */
+    int32_t  inverse;         /* 1: turned back (by -angle): the gradient of the turn                       */
+    double   magnitude;       /* the turned pairs are multiplied by it; finite                              */
+    int32_t  page_size;       /* with a cache                                                               */
+    int32_t  reserved;        /* must be 0                                                                  */
+    int64_t  cache_pages;     /* with a cache                                                               */
+    /* elements between tokens and between heads of a token; a head's dimensions are consecutive          */
+    int64_t  q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+    int64_t  q_out_stride, q_out_head_stride, k_out_stride, k_out_head_stride;
+} ciar_rotary_params;
+
+/*
+ * Rotary positions: pair p of every head of token t is turned by the angle positions[t] * inv_freq[p] (in 64 bits) and
+ * multiplied by `magnitude`: (a, b) -> m (a cos - b sin, b cos + a sin); dimensions from rotary_dim on are copied.
+ *   q [T, q_heads, D], k [T, kv_heads, D]  in      positions [T] int32, inv_freq [rotary_dim / 2] double  in
+ *   q_out [T, q_heads, D]                  out     k_out [T, kv_heads, D]  out, without a cache
+ * With a cache (k_cache, v_cache, slots and v [T, kv_heads, D] all given, k_out NULL) the turned keys and the values go to
+ * slots [T] int32 of the cache instead; a slot outside the cache is left out (-1: a token without a place), and no slot may come twice.
+ * Outputs must not overlap inputs.  Any alignment of q, k, v and their outputs; caches 16-byte aligned.
+ */
+int ciar_rotary(const void* q, const void* k, const void* v, const int32_t* positions, const double* inv_freq, int64_t T,
+                const ciar_rotary_params* params, void* q_out, void* k_out, void* k_cache, void* v_cache,
+                const int32_t* slots, void* hip_stream);
+
+typedef struct ciar_attention_params {
+    uint32_t struct_size;     /* sizeof(ciar_attention_params); checked                                     */
+    int32_t  q_heads, kv_heads;   /* q_heads a multiple of kv_heads: query head h reads head h / (q_heads / kv_heads) */
+    int32_t  head_dim;        /* a multiple of 32, 32 to 256                                                */
+    int32_t  page_size;
+    int32_t  table_width;     /* columns of a request's row of pages                                        */
+    int32_t  max_new;         /* no request has more new tokens                                             */
+    int32_t  max_len;         /* no request has more tokens in the cache                                    */
+    float    scale;           /* of the scores; finite                                                      */
+    int32_t  reserved;        /* must be 0                                                                  */
+    int64_t  table_stride, cache_pages;
+    int64_t  q_stride, q_head_stride, out_stride, out_head_stride;
+} ciar_attention_params;
+
+/* Bytes of device workspace ciar_paged_attention needs for R requests and T new tokens (0: none). */
+size_t ciar_attention_workspace_bytes(int64_t R, int64_t T, const ciar_attention_params* params);
+
+/*
+ * Attention over the paged cache.  Request r's new tokens are the rows cu_new[r] .. cu_new[r + 1] - 1 of q; their keys and
+ * values are already in the cache, whose first kv_len[r] tokens of request r lie in the pages table[r][0 ...].  The j-th of n
+ * new tokens stands at position kv_len[r] - n + j and sees the positions up to its own:
+ *   s_i = scale q . k_i,  lse = ln sum_i exp(s_i),  out = sum_i exp(s_i - lse) v_i,     i = 0 .. kv_len[r] - n + j
+ * A row that sees nothing (kv_len 0: a request that was not granted; rows that belong to no request) has out = 0 and
+ * lse = -inf.  Scores, their maximum and sum and the output are kept in 32 bits; the weights exp(s_i - running maximum) are
+ * rounded to bfloat16 for the second product.  What slots beyond a row's last position hold (infinities and NaN included) has no
+ * effect on it.
+ *   q [T, q_heads, D] bf16  in      table [R, table_width] int32, cu_new [R + 1], kv_len [R] int32  in
+ *   out [T, q_heads, D] bf16, lse [T, q_heads] float  out (lse may be NULL)
+ * table entries are clamped into the cache, kv_len into [0, min(max_len, table_width * page_size)] and cu_new into [0, T].
+ */
+int ciar_paged_attention(const void* q, const void* k_cache, const void* v_cache, const int32_t* table,
+                         const int32_t* cu_new, const int32_t* kv_len, int64_t R, int64_t T,
+                         const ciar_attention_params* params, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * What ciar_adjust_logits applies; row n of N belongs to request (window) r = n / params->window.  Every pointer is a device
+ * pointer; a group whose pointers are NULL is left out.
+ */
+typedef struct ciar_adjustments {
+    uint32_t struct_size;             /* sizeof(ciar_adjustments); checked                                     */
+    int32_t  mask_rows;               /* rows of `allowed`                                                     */
+    /* tokens so far: request r's are history[history_start[r] .. history_start[r + 1] - 1], the first prompt_len[r] of
+     * them the prompt (NULL: none); row n's also end with the drafted tokens of its window before it */
+    const int64_t* history_start;     /* [W + 1], W = ceil(N / window)                                         */
+    const int32_t* history;           /* [history_len]                                                         */
+    int64_t        history_len;
+    const int32_t* prompt_len;        /* [W]                                                                   */
+    const int32_t* drafted;           /* [N]: the drafted token of each row                                    */
+    const float*   repetition;        /* [W] > 0                                                               */
+    const float*   presence;          /* [W]                                                                   */
+    const float*   frequency;         /* [W]                                                                   */
+    const int64_t* bias_start;        /* [W + 1]                                                               */
+    const int32_t* bias_ids;          /* [bias_len], ascending within a request (equal ones add up)            */
+    const float*   bias_values;       /* [bias_len]                                                            */
+    int64_t        bias_len;
+    const int32_t* allowed;           /* [mask_rows, allowed_stride]: bit t % 32 of word t / 32 set = token t allowed */
+    int64_t        allowed_stride;    /* words                                                                 */
+    const int32_t* allowed_row;       /* [N]: the row's mask; negative = none                                  */
+} ciar_adjustments;
+
+size_t ciar_adjust_workspace_bytes(int64_t N, const ciar_params* params);
+
+/*
+ * Penalties, biases and grammar masks on logits, in 32 bits, rounded once.  For token t of row n, with ever = t occurs among
+ * the row's tokens so far and c = how often it does behind the prompt:
+ *   x <- ever ? (x > 0 ? x / repetition : x * repetition) : x
+ *   x <- x - frequency c - presence [c > 0]
+ *   x <- x + bias(t)
+ *   x <- allowed(t) ? x : -inf
+ *   logits [N, row_stride]  in      out [N, out_stride]  out, may be `logits` itself (same stride), must not overlap it otherwise
+ *   left [N] int32          out     finite logits left in the row (0: nothing is allowed); may be NULL
+ * params: vocab, dtype, window, row_stride (rules as above, for `out` too; only the V logits of a row are written).
+ * Tokens outside the vocabulary count for nothing; offsets are clamped into their arrays and mask rows into `allowed`.
+ * workspace: ciar_adjust_workspace_bytes(N, params) bytes if `left` is given; no initialisation (see ciar_workspace_bytes).
+ */
+int ciar_adjust_logits(const void* logits, int64_t N, const ciar_params* params, const ciar_adjustments* adjust,
+                       void* out, int64_t out_stride, int32_t* left, void* workspace, size_t workspace_bytes,
+                       void* hip_stream);
+
 /*
  * Window epilogue on its own (the last step of ciar_verify / ciar_quantify_verify, which run it when
  * a window output is requested): from the per-row results of N rows,

@@ -1,14 +1,19 @@
 """MI355X-native CIAR quantify + verify hot path: HIP kernels behind a C ABI, with a thin binding.
 
 ``binding`` marshals torch tensors into the C ABI declared in ``include/ciar.h``;
-``workloads`` generates the seeded synthetic inputs; ``build`` compiles ``libciar.so`` for gfx950.
+``step`` does so for the operators of the verification step around the accept test (cache plan, rotary positions, paged
+attention, the logits' adjustments); ``workloads`` generates the seeded synthetic inputs; ``build`` compiles ``libciar.so`` for gfx950.
 """
 from .binding import (DRO_LOSSES, DRO_TERMS, ENSEMBLE, VOTING, CiarError, Params, dense_intervals,
                       finish_rows, interdro_loss, interhead_logits, interhead_quantify, last_error, lib, quantify, quantify_multihead,
                       quantify_verify, quantify_verify_static, read_rows, stream_rows, verify, version, window_epilogue,
                       workspace_bytes)
+from .step import (adjust_logits, adjust_workspace_bytes, attention_workspace_bytes, cache_plan, cache_shapes, paged_attention,
+                   rotary)
 
 __all__ = ["DRO_LOSSES", "DRO_TERMS", "ENSEMBLE", "VOTING", "CiarError", "Params", "dense_intervals",
            "finish_rows", "interdro_loss", "interhead_logits", "interhead_quantify", "last_error", "lib", "quantify", "quantify_multihead",
            "quantify_verify", "quantify_verify_static", "read_rows", "stream_rows", "verify", "version", "window_epilogue",
-           "workspace_bytes"]
+           "workspace_bytes",
+           "adjust_logits", "adjust_workspace_bytes", "attention_workspace_bytes", "cache_plan", "cache_shapes",
+           "paged_attention", "rotary"]

@@ -93,6 +93,19 @@ def lib() -> ctypes.CDLL:
         L.ciar_interhead_logits_timed.argtypes = [vp, vp, vp, ctypes.c_int32, i64, pp, vp, vp, vp, vp, vp]
         L.ciar_interhead_quantify.restype = ctypes.c_int
         L.ciar_interhead_quantify.argtypes = [vp, vp, vp, ctypes.c_int32, vp, i64, pp] + [vp] * 7 + [vp, sz, vp]
+        i32 = ctypes.c_int32
+        L.ciar_cache_plan.restype = ctypes.c_int
+        L.ciar_cache_plan.argtypes = [vp] * 4 + [i64, vp, i64, vp, vp, i32, i64, i32, i64] + [vp] * 9 + [vp]
+        L.ciar_rotary.restype = ctypes.c_int
+        L.ciar_rotary.argtypes = [vp] * 5 + [i64, vp] + [vp] * 5 + [vp]
+        L.ciar_attention_workspace_bytes.restype = sz
+        L.ciar_attention_workspace_bytes.argtypes = [i64, i64, vp]
+        L.ciar_paged_attention.restype = ctypes.c_int
+        L.ciar_paged_attention.argtypes = [vp] * 6 + [i64, i64, vp, vp, vp, vp, sz, vp]
+        L.ciar_adjust_workspace_bytes.restype = sz
+        L.ciar_adjust_workspace_bytes.argtypes = [i64, pp]
+        L.ciar_adjust_logits.restype = ctypes.c_int
+        L.ciar_adjust_logits.argtypes = [vp, i64, pp, vp, vp, i64, vp, vp, sz, vp]
         L.ciar_width_polynomial.restype = ctypes.c_int
         L.ciar_width_polynomial.argtypes = [pp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_float)]
         L.ciar_last_error.restype = ctypes.c_char_p

@@ -8,8 +8,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libciar.so")
-SOURCES = ["ciar_stream.hip", "ciar_rows.hip", "ciar_short.hip", "ciar_radius.hip", "ciar_finish.hip", "ciar_heads.hip", "ciar_loss.hip", "ciar_aux.hip", "ciar_interhead.hip", "ciar_api.cpp"]
-HEADERS = ["ciar_internal.h", "ciar_device.h", "ciar_stream.h", os.path.join("..", "..", "include", "ciar.h")]
+SOURCES = ["ciar_stream.hip", "ciar_rows.hip", "ciar_short.hip", "ciar_radius.hip", "ciar_finish.hip", "ciar_heads.hip", "ciar_loss.hip", "ciar_aux.hip", "ciar_interhead.hip", "ciar_plan.hip", "ciar_rotary.hip", "ciar_attention.hip", "ciar_logits.hip", "ciar_api.cpp", "ciar_step.cpp"]
+HEADERS = ["ciar_internal.h", "ciar_host.h", "ciar_step.h", "ciar_device.h", "ciar_stream.h", os.path.join("..", "..", "include", "ciar.h")]
 
 # Packed-FP32 instructions are switched off for every device compile of this library.
 HIPCC_FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

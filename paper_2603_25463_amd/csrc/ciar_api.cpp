@@ -3,6 +3,7 @@
 // for ciar_quantify_verify_static, the addresses of the built-in scratch buffer.
 #include "../../include/ciar.h"
 #include "ciar_internal.h"
+#include "ciar_host.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -13,17 +14,42 @@
 #include <mutex>
 
 namespace {
-
 thread_local char g_error[512] = "";
+}  // namespace
 
-int fail(ciar_status code, const char* fmt, ...)
+namespace ciar {
+
+int fail(int code, const char* fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_error, sizeof g_error, fmt, ap);
     va_end(ap);
-    return (int)code;
+    return code;
 }
+
+int hip_fail(hipError_t e, const char* what)
+{
+    return fail(CIAR_EHIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+uint32_t next_tag()
+{
+    static std::atomic<uint32_t> tag{(uint32_t)std::chrono::steady_clock::now().time_since_epoch().count() * 2654435761u};
+    for (;;) {
+        const uint32_t t = tag.fetch_add(1, std::memory_order_relaxed) + 1;
+        if ((t & 0x7fffffffu) != 0) return t;                      // (a zero tag marks a word that has been handed back)
+    }
+}
+
+}  // namespace ciar
+
+namespace {
+
+using ciar::fail;
+using ciar::hip_fail;
+using ciar::next_tag;
+using ciar::discard_stale_hip_error;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -50,8 +76,9 @@ struct Resolved {
     int elt;           // bytes per logit
 };
 
-// Checks everything in `p` that does not depend on the tensors.  Returns CIAR_OK or fails.
-int check_params(const ciar_params* p, Resolved* out)
+}  // namespace
+
+int ciar::check_row_params(const ciar_params* p)
 {
     if (!p) return fail(CIAR_EINVAL, "params is NULL");
     if (p->struct_size != sizeof(ciar_params))
@@ -71,6 +98,15 @@ int check_params(const ciar_params* p, Resolved* out)
         return fail(CIAR_EALIGN, "row_stride * element size = %lld bytes is not a multiple of 16",
                     (long long)(p->row_stride * elt));
     if (p->window < 1) return fail(CIAR_EINVAL, "params->window must be >= 1 (got %d)", p->window);
+    return CIAR_OK;
+}
+
+namespace {
+
+// Checks everything in `p` that does not depend on the tensors.  Returns CIAR_OK or fails.
+int check_params(const ciar_params* p, Resolved* out)
+{
+    if (int rc = ciar::check_row_params(p)) return rc;
     if (!(p->radius_max >= 0.0f) || !(p->radius_max <= 16.0f))
         return fail(CIAR_EINVAL, "params->radius_max must be in [0, 16] (got %g)", (double)p->radius_max);
     if (!std::isfinite(p->tau)) return fail(CIAR_EINVAL, "params->tau must be finite");
@@ -90,7 +126,7 @@ int check_params(const ciar_params* p, Resolved* out)
     out->a = std::exp(r);
     out->b = std::exp(-r);
     out->kappa = kappa;
-    out->elt = elt;
+    out->elt = p->dtype == CIAR_F32 ? 4 : 2;
     return CIAR_OK;
 }
 
@@ -194,16 +230,6 @@ ciar::RowArgs base_args(const ciar_params* p, const Resolved& r, int64_t N)
     return a;
 }
 
-int hip_fail(hipError_t e, const char* what)
-{
-    return fail(CIAR_EHIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-// The launchers report hipGetLastError() after a launch.  HIP keeps that state per host thread and a successful call
-// does not reset it, so an error left by an earlier, unrelated call of the thread is discarded before the first
-// launch of an entry point: what is reported afterwards is this call's.
-void discard_stale_hip_error() { (void)hipGetLastError(); }
-
 // Workspace layout: [N] RowStats | [N] int32 row ids | [N] int32 arg-max tokens | 16 B (unused) | [N] uint8 accept bits
 // (rounded up to 128 B) | 16 N bytes for the words of windows that span workgroups: window w at byte 16 K w, so that
 // from K = 8 on every window has a 128-byte line of its own (the rows of many windows arrive at once, and atomic
@@ -301,18 +327,6 @@ int fill(const Call& c, ciar::Mode mode, ciar::RowArgs* a)
 // Tensor mode reports the arg-max token's interval with that token's own radius: without drafted ids the index
 // comes from a kernel of its own, into a workspace array of N ints.
 bool needs_argmax(const ciar::RowArgs& a) { return a.radius && !a.ids && (a.p_lo || a.p_hi); }
-
-// Tags for the words the streaming kernel keeps in caller memory (see window_arrive in ciar_device.h): a different
-// one for every launch of the process, starting from a value that varies from run to run.  (A captured graph replays
-// a launch with its tag: the kernel hands every word back, with a zero tag, when a window is complete.)
-uint32_t next_tag()
-{
-    static std::atomic<uint32_t> tag{(uint32_t)std::chrono::steady_clock::now().time_since_epoch().count() * 2654435761u};
-    for (;;) {
-        const uint32_t t = tag.fetch_add(1, std::memory_order_relaxed) + 1;
-        if ((t & 0x7fffffffu) != 0) return t;                      // (a zero tag marks a word that has been handed back)
-    }
-}
 
 // Stage 1: the streaming kernel, which also finishes its rows (and the fp64 pass over flat rows where the call needs it).
 int run_stream(const Call& c, ciar::Mode mode)

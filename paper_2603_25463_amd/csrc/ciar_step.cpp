@@ -1,0 +1,344 @@
+// C ABI of the verification step around the accept test (include/ciar.h): validation and launches of the cache plan, the
+// rotary positions, the attention over the paged cache and the logits' adjustments.  No allocation, no synchronisation.
+#include "../../include/ciar.h"
+#include "ciar_step.h"
+#include "ciar_host.h"
+
+#include <cmath>
+#include <cstring>
+
+namespace {
+
+using ciar::fail;
+using ciar::hip_fail;
+
+constexpr int64_t kMost = 0x7fffffffLL;
+
+// A piece of memory [first, last) that a call touches.
+struct Span { uintptr_t first, last; };
+
+Span span_of(const void* p, int64_t bytes)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return {a, a + (uintptr_t)(p && bytes > 0 ? bytes : 0)};
+}
+bool meet(const Span& a, const Span& b) { return a.first < b.last && b.first < a.last; }
+
+Span span_of(const ciar::Heads& h, int64_t T, int heads, int D, int elt)
+{
+    return span_of(h.p, T > 0 ? ((T - 1) * h.token + (heads - 1) * h.head + D) * (int64_t)elt : 0);
+}
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// [T, heads, D] of `elt`-byte elements whose strides do not run backwards (and, for an output, do not fold rows onto each other).
+int check_heads(const ciar::Heads& h, int64_t T, int heads, int D, int elt, bool output, const char* name)
+{
+    if (!h.p) return fail(CIAR_EINVAL, "%s is NULL", name);
+    if (!aligned(h.p, (uintptr_t)elt)) return fail(CIAR_EALIGN, "%s is not aligned to its elements", name);
+    if (h.token < 0 || h.head < 0) return fail(CIAR_EINVAL, "%s has a negative stride", name);
+    if (h.token > (1LL << 40) || h.head > (1LL << 40)) return fail(CIAR_EUNSUPPORTED, "%s has a stride above 2^40", name);
+    if (output) {
+        const bool inner = heads == 1 || h.head >= D, outer = T <= 1 || h.token >= D;
+        // rows of a token side by side within a token, or tokens of a head side by side within a head
+        const bool apart = T <= 1 || heads == 1 || h.token >= (heads - 1) * h.head + D || h.head >= (T - 1) * h.token + D;
+        if (!inner || !outer || !apart) return fail(CIAR_EINVAL, "%s: rows overlap", name);
+    }
+    return CIAR_OK;
+}
+
+int check_heads_of(int32_t q_heads, int32_t kv_heads)
+{
+    if (q_heads < 1 || kv_heads < 1) return fail(CIAR_EINVAL, "q_heads and kv_heads must be >= 1 (got %d, %d)", q_heads, kv_heads);
+    if (q_heads > 65535 || kv_heads > 65535) return fail(CIAR_EUNSUPPORTED, "more than 65535 heads");
+    return CIAR_OK;
+}
+
+int check_pages(int32_t page_size, int64_t pages, const char* what)
+{
+    if (page_size < ciar::kAtom || page_size % ciar::kAtom != 0)
+        return fail(CIAR_EUNSUPPORTED, "page_size %d is not a positive multiple of %d", page_size, ciar::kAtom);
+    if (pages < 1) return fail(CIAR_EINVAL, "%s must be >= 1", what);
+    if (pages > kMost / page_size) return fail(CIAR_EUNSUPPORTED, "%s * page_size exceeds 2^31 - 1 slots", what);
+    return CIAR_OK;
+}
+
+int64_t cache_bytes(int64_t pages, int32_t page, int32_t heads, int32_t D) { return pages * page * (int64_t)heads * D * 2; }
+
+}  // namespace
+
+extern "C" {
+
+int ciar_cache_plan(const int32_t* lengths, const int32_t* kept, const int32_t* new_tokens, const int32_t* held, int64_t R,
+                    int32_t* ring, int64_t ring_pages, const int64_t* ring_state, int32_t* table, int32_t table_width,
+                    int64_t table_stride, int32_t page_size, int64_t T, int32_t* out_lengths, int32_t* kv_len,
+                    int32_t* cu_new, int32_t* out_held, uint8_t* granted, int64_t* out_ring_state, int32_t* slots,
+                    int32_t* positions, int32_t* requests, void* hip_stream)
+{
+    if (R < 0 || T < 0) return fail(CIAR_EINVAL, "R or T is negative");
+    if (R > kMost || T >= kMost) return fail(CIAR_EUNSUPPORTED, "R or T exceeds 2^31 - 2");
+    if (int rc = check_pages(page_size, ring_pages, "ring_pages")) return rc;
+    if (table_width < 1) return fail(CIAR_EINVAL, "table_width must be >= 1 (got %d)", table_width);
+    if (table_width > kMost / page_size) return fail(CIAR_EUNSUPPORTED, "table_width * page_size exceeds 2^31 - 1 positions");
+    if (R > 1 && table_stride < table_width) return fail(CIAR_EINVAL, "table_stride is smaller than table_width");
+    if (table_stride > kMost) return fail(CIAR_EUNSUPPORTED, "table_stride exceeds 2^31 - 1");
+    if (!ring || !ring_state) return fail(CIAR_EINVAL, "ring or ring_state is NULL");
+    if (R > 0 && !(lengths && new_tokens && held && table)) return fail(CIAR_EINVAL, "lengths, new_tokens, held or table is NULL");
+    if (R > 0 && !(out_lengths && kv_len && out_held && granted)) return fail(CIAR_EINVAL, "out_lengths, kv_len, out_held or granted is NULL");
+    if (!cu_new || !out_ring_state) return fail(CIAR_EINVAL, "cu_new or out_ring_state is NULL");
+    if (T > 0 && !(slots && positions && requests)) return fail(CIAR_EINVAL, "slots, positions or requests is NULL");
+    const Span in[] = {span_of(lengths, R * 4), span_of(kept, R * 4), span_of(new_tokens, R * 4), span_of(held, R * 4),
+                       span_of(ring_state, 16)};
+    const Span out[] = {span_of(ring, ring_pages * 4), span_of(table, R > 0 ? ((R - 1) * table_stride + table_width) * 4 : 0),
+                        span_of(out_lengths, R * 4), span_of(kv_len, R * 4), span_of(cu_new, (R + 1) * 4), span_of(out_held, R * 4),
+                        span_of(granted, R), span_of(out_ring_state, 16), span_of(slots, T * 4), span_of(positions, T * 4),
+                        span_of(requests, T * 4)};
+    constexpr int nout = sizeof out / sizeof out[0];
+    for (int i = 0; i < nout; ++i) {
+        for (const Span& x : in)
+            if (meet(out[i], x)) return fail(CIAR_EINVAL, "an output of the plan overlaps an input");
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return fail(CIAR_EINVAL, "two outputs of the plan overlap");
+    }
+    ciar::PlanArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.lengths = lengths; a.kept = kept; a.fresh = new_tokens; a.held = held;
+    a.ring = ring; a.ring_state = ring_state; a.table = table; a.table_stride = table_stride;
+    a.R = (int32_t)R; a.P = (int32_t)ring_pages; a.width = table_width; a.page = page_size; a.T = (int32_t)T;
+    a.out_lengths = out_lengths; a.kv_len = kv_len; a.cu_new = cu_new; a.out_held = out_held; a.granted = granted;
+    a.out_ring_state = out_ring_state; a.slots = slots; a.positions = positions; a.requests = requests;
+    ciar::discard_stale_hip_error();
+    const hipError_t e = ciar::launch_plan(a, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return hip_fail(e, "plan kernel launch");
+    return CIAR_OK;
+}
+
+int ciar_rotary(const void* q, const void* k, const void* v, const int32_t* positions, const double* inv_freq, int64_t T,
+                const ciar_rotary_params* p, void* q_out, void* k_out, void* k_cache, void* v_cache, const int32_t* slots,
+                void* hip_stream)
+{
+    if (!p) return fail(CIAR_EINVAL, "params is NULL");
+    if (p->struct_size != sizeof(ciar_rotary_params))
+        return fail(CIAR_EINVAL, "params->struct_size is %u, expected %zu", p->struct_size, sizeof(ciar_rotary_params));
+    if (p->reserved != 0) return fail(CIAR_EINVAL, "params->reserved must be 0");
+    if (p->dtype != CIAR_F32 && p->dtype != CIAR_BF16)
+        return fail(CIAR_EUNSUPPORTED, "params->dtype %d is neither CIAR_F32 nor CIAR_BF16", p->dtype);
+    if (int rc = check_heads_of(p->q_heads, p->kv_heads)) return rc;
+    if (p->head_dim < 2 || p->rotary_dim < 2 || p->rotary_dim > p->head_dim || p->rotary_dim % 2 != 0)
+        return fail(CIAR_EINVAL, "rotary_dim %d must be even and in [2, head_dim %d]", p->rotary_dim, p->head_dim);
+    if (p->rotary_dim > 1024 || p->head_dim > 65536)
+        return fail(CIAR_EUNSUPPORTED, "rotary_dim above 1024 or head_dim above 65536 (got %d, %d)", p->rotary_dim, p->head_dim);
+    if (!std::isfinite(p->magnitude)) return fail(CIAR_EINVAL, "params->magnitude is not finite");
+    if (T < 0) return fail(CIAR_EINVAL, "T is negative");
+    if (T > kMost) return fail(CIAR_EUNSUPPORTED, "T exceeds 2^31 - 1");
+    const bool cached = k_cache || v_cache || slots;
+    if (cached) {
+        if (!k_cache || !v_cache || !slots) return fail(CIAR_EINVAL, "k_cache, v_cache and slots go together");
+        if (k_out) return fail(CIAR_EINVAL, "k_out is not written where a cache is given");
+        if (p->dtype != CIAR_BF16) return fail(CIAR_EUNSUPPORTED, "the cache holds bfloat16: params->dtype must be CIAR_BF16");
+        if (p->head_dim % 8 != 0) return fail(CIAR_EUNSUPPORTED, "head_dim %d is not a multiple of 8, as the cache needs", p->head_dim);
+        if (int rc = check_pages(p->page_size, p->cache_pages, "cache_pages")) return rc;
+        if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return fail(CIAR_EALIGN, "k_cache or v_cache is not 16-byte aligned");
+    } else if (v) {
+        return fail(CIAR_EINVAL, "v is given without a cache");
+    }
+    if (T == 0) return CIAR_OK;
+    if (!positions || !inv_freq) return fail(CIAR_EINVAL, "positions or inv_freq is NULL");
+    const int elt = p->dtype == CIAR_F32 ? 4 : 2, D = p->head_dim;
+    ciar::RotaryArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.q = {q, p->q_stride, p->q_head_stride};
+    a.k = {k, p->k_stride, p->k_head_stride};
+    a.v = {v, p->v_stride, p->v_head_stride};
+    a.q_out = {q_out, p->q_out_stride, p->q_out_head_stride};
+    a.k_out = {k_out, p->k_out_stride, p->k_out_head_stride};
+    if (int rc = check_heads(a.q, T, p->q_heads, D, elt, false, "q")) return rc;
+    if (int rc = check_heads(a.k, T, p->kv_heads, D, elt, false, "k")) return rc;
+    if (int rc = check_heads(a.q_out, T, p->q_heads, D, elt, true, "q_out")) return rc;
+    Span out[3] = {span_of(a.q_out, T, p->q_heads, D, elt), {0, 0}, {0, 0}};
+    if (cached) {
+        if (int rc = check_heads(a.v, T, p->kv_heads, D, elt, false, "v")) return rc;
+        const int64_t bytes = cache_bytes(p->cache_pages, p->page_size, p->kv_heads, D);
+        out[1] = span_of(k_cache, bytes);
+        out[2] = span_of(v_cache, bytes);
+    } else {
+        if (int rc = check_heads(a.k_out, T, p->kv_heads, D, elt, true, "k_out")) return rc;
+        out[1] = span_of(a.k_out, T, p->kv_heads, D, elt);
+    }
+    const Span in[] = {span_of(a.q, T, p->q_heads, D, elt), span_of(a.k, T, p->kv_heads, D, elt),
+                       span_of(a.v, v ? T : 0, p->kv_heads, D, elt), span_of(positions, T * 4), span_of(inv_freq, p->rotary_dim * 4),
+                       span_of(slots, T * 4)};
+    // (rows of q_out and k_out may lie side by side in one tensor: those two are told apart row by row, as strided tensors are not)
+    for (const Span& o : out)
+        for (const Span& x : in)
+            if (meet(o, x)) return fail(CIAR_EINVAL, "an output overlaps an input");
+    if (meet(out[1], out[2]) || (cached && (meet(out[0], out[1]) || meet(out[0], out[2]))))
+        return fail(CIAR_EINVAL, "two outputs overlap");
+    a.positions = positions;
+    a.inv_freq = inv_freq;
+    a.k_cache = k_cache; a.v_cache = v_cache; a.slots = slots;
+    a.magnitude = p->magnitude;
+    a.sign = p->inverse ? -1.0 : 1.0;
+    a.slot_count = cached ? p->cache_pages * p->page_size : 0;
+    a.T = (int32_t)T; a.q_heads = p->q_heads; a.kv_heads = p->kv_heads; a.D = D; a.n = p->rotary_dim;
+    a.page = cached ? p->page_size : ciar::kAtom;
+    ciar::discard_stale_hip_error();
+    const hipError_t e = ciar::launch_rotary(p->dtype, p->interleaved != 0, a, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return hip_fail(e, "rotary kernel launch");
+    return CIAR_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Checks the sizes of an attention call and fills them in.
+int attention_args(int64_t R, int64_t T, const ciar_attention_params* p, ciar::AttentionArgs* a)
+{
+    if (!p) return fail(CIAR_EINVAL, "params is NULL");
+    if (p->struct_size != sizeof(ciar_attention_params))
+        return fail(CIAR_EINVAL, "params->struct_size is %u, expected %zu", p->struct_size, sizeof(ciar_attention_params));
+    if (p->reserved != 0) return fail(CIAR_EINVAL, "params->reserved must be 0");
+    if (int rc = check_heads_of(p->q_heads, p->kv_heads)) return rc;
+    if (p->q_heads % p->kv_heads != 0)
+        return fail(CIAR_EINVAL, "q_heads %d is not a multiple of kv_heads %d", p->q_heads, p->kv_heads);
+    if (p->head_dim < 32 || p->head_dim > 256 || p->head_dim % 32 != 0)
+        return fail(CIAR_EUNSUPPORTED, "head_dim %d is not a multiple of 32 in [32, 256]", p->head_dim);
+    if (int rc = check_pages(p->page_size, p->cache_pages, "cache_pages")) return rc;
+    if (p->table_width < 1) return fail(CIAR_EINVAL, "table_width must be >= 1 (got %d)", p->table_width);
+    if (p->table_width > kMost / p->page_size) return fail(CIAR_EUNSUPPORTED, "table_width * page_size exceeds 2^31 - 1 positions");
+    if (p->max_new < 0 || p->max_len < 0) return fail(CIAR_EINVAL, "max_new or max_len is negative");
+    if (!std::isfinite(p->scale)) return fail(CIAR_EINVAL, "params->scale is not finite");
+    if (R < 0 || T < 0) return fail(CIAR_EINVAL, "R or T is negative");
+    if (R > 65535) return fail(CIAR_EUNSUPPORTED, "R exceeds 65535 requests per call");
+    if (T > kMost / p->q_heads) return fail(CIAR_EUNSUPPORTED, "T * q_heads exceeds 2^31 - 1 rows");
+    if (R > 1 && p->table_stride < p->table_width) return fail(CIAR_EINVAL, "table_stride is smaller than table_width");
+    if (p->table_stride < 0 || p->table_stride > kMost) return fail(CIAR_EUNSUPPORTED, "table_stride is outside [0, 2^31 - 1]");
+    std::memset(a, 0, sizeof *a);
+    a->scale = p->scale;
+    a->table_stride = p->table_stride;
+    a->R = (int32_t)R; a->T = (int32_t)T; a->q_heads = p->q_heads; a->kv_heads = p->kv_heads; a->D = p->head_dim;
+    a->page = p->page_size; a->pages = (int32_t)p->cache_pages; a->width = p->table_width;
+    // no request has more rows than there are, nor more tokens than its row of pages holds
+    a->max_new = p->max_new < T ? p->max_new : (int32_t)T;
+    a->max_len = p->max_len < p->table_width * p->page_size ? p->max_len : p->table_width * p->page_size;
+    return CIAR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ciar_attention_workspace_bytes(int64_t R, int64_t T, const ciar_attention_params* p)
+{
+    ciar::AttentionArgs a;
+    if (R <= 0 || T <= 0 || attention_args(R, T, p, &a) != CIAR_OK) return 0;
+    return (ciar::attention_workspace(a) + 255) / 256 * 256;
+}
+
+int ciar_paged_attention(const void* q, const void* k_cache, const void* v_cache, const int32_t* table,
+                         const int32_t* cu_new, const int32_t* kv_len, int64_t R, int64_t T,
+                         const ciar_attention_params* p, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                         void* hip_stream)
+{
+    ciar::AttentionArgs a;
+    if (int rc = attention_args(R, T, p, &a)) return rc;
+    if (T == 0) return CIAR_OK;
+    a.q = {q, p->q_stride, p->q_head_stride};
+    a.out = {out, p->out_stride, p->out_head_stride};
+    if (int rc = check_heads(a.q, T, p->q_heads, p->head_dim, 2, false, "q")) return rc;
+    if (int rc = check_heads(a.out, T, p->q_heads, p->head_dim, 2, true, "out")) return rc;
+    if (R > 0 && !(table && kv_len)) return fail(CIAR_EINVAL, "table or kv_len is NULL");
+    if (!cu_new) return fail(CIAR_EINVAL, "cu_new is NULL");
+    if (!k_cache || !v_cache) return fail(CIAR_EINVAL, "k_cache or v_cache is NULL");
+    if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return fail(CIAR_EALIGN, "k_cache or v_cache is not 16-byte aligned");
+    const int64_t bytes = cache_bytes(p->cache_pages, p->page_size, p->kv_heads, p->head_dim);
+    const Span o[] = {span_of(a.out, T, p->q_heads, p->head_dim, 2), span_of(lse, T * p->q_heads * 4)};
+    const Span in[] = {span_of(a.q, T, p->q_heads, p->head_dim, 2), span_of(k_cache, bytes), span_of(v_cache, bytes),
+                       span_of(table, R > 0 ? ((R - 1) * p->table_stride + p->table_width) * 4 : 0),
+                       span_of(cu_new, (R + 1) * 4), span_of(kv_len, R * 4)};
+    for (const Span& x : o)
+        for (const Span& y : in)
+            if (meet(x, y)) return fail(CIAR_EINVAL, "an output overlaps an input");
+    if (meet(o[0], o[1])) return fail(CIAR_EINVAL, "out and lse overlap");
+    const size_t need = ciar::attention_workspace(a);
+    if (need > 0) {
+        if (!workspace) return fail(CIAR_EWORKSPACE, "workspace is NULL but %zu bytes are needed", need);
+        if (!aligned(workspace, 16)) return fail(CIAR_EALIGN, "workspace is not 16-byte aligned");
+        if (workspace_bytes < need) return fail(CIAR_EWORKSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, need);
+    }
+    a.k_cache = k_cache; a.v_cache = v_cache; a.table = table; a.cu_new = cu_new; a.kv_len = kv_len; a.lse = lse;
+    ciar::discard_stale_hip_error();
+    const hipError_t e = ciar::launch_attention(a, need > 0 ? workspace : nullptr, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
+    return CIAR_OK;
+}
+
+size_t ciar_adjust_workspace_bytes(int64_t N, const ciar_params* params)
+{
+    if (N <= 0 || !params) return 0;
+    return ((size_t)N * 8 + 255) / 256 * 256;
+}
+
+int ciar_adjust_logits(const void* logits, int64_t N, const ciar_params* params, const ciar_adjustments* j, void* out,
+                       int64_t out_stride, int32_t* left, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (int rc = ciar::check_row_params(params)) return rc;
+    if (!j) return fail(CIAR_EINVAL, "adjust is NULL");
+    if (j->struct_size != sizeof(ciar_adjustments))
+        return fail(CIAR_EINVAL, "adjust->struct_size is %u, expected %zu", j->struct_size, sizeof(ciar_adjustments));
+    if (N < 0) return fail(CIAR_EINVAL, "N is negative");
+    if (N > kMost) return fail(CIAR_EUNSUPPORTED, "N exceeds 2^31 - 1 rows per call");
+    const int elt = params->dtype == CIAR_F32 ? 4 : 2;
+    if (out_stride < params->vocab) return fail(CIAR_EINVAL, "out_stride is smaller than vocab %d", params->vocab);
+    if (out_stride * elt % 16 != 0) return fail(CIAR_EALIGN, "out_stride is not a multiple of 16 bytes");
+    if ((j->history_start != nullptr) != (j->history != nullptr) || (j->prompt_len && !j->history_start))
+        return fail(CIAR_EINVAL, "history_start and history go together, and prompt_len needs them");
+    if ((j->bias_start != nullptr) != (j->bias_ids != nullptr) || (j->bias_ids != nullptr) != (j->bias_values != nullptr))
+        return fail(CIAR_EINVAL, "bias_start, bias_ids and bias_values go together");
+    if ((j->allowed != nullptr) != (j->allowed_row != nullptr)) return fail(CIAR_EINVAL, "allowed and allowed_row go together");
+    if (j->history_len < 0 || j->bias_len < 0) return fail(CIAR_EINVAL, "history_len or bias_len is negative");
+    if (j->allowed && (j->mask_rows < 1 || j->allowed_stride < (params->vocab + 31) / 32))
+        return fail(CIAR_EINVAL, "allowed needs a row and %d words a row (mask_rows %d, allowed_stride %lld)",
+                    (params->vocab + 31) / 32, j->mask_rows, (long long)j->allowed_stride);
+    if (N == 0) return CIAR_OK;
+    if (!logits || !out) return fail(CIAR_EINVAL, "logits or out is NULL");
+    if (!aligned(logits, 16) || !aligned(out, 16)) return fail(CIAR_EALIGN, "logits or out is not 16-byte aligned");
+    const int64_t V = params->vocab, W = (N + params->window - 1) / params->window;
+    const Span o[] = {span_of(out, ((N - 1) * out_stride + V) * elt), span_of(left, N * 4)};
+    const Span in[] = {span_of(j->history_start, (W + 1) * 8), span_of(j->history, j->history_len * 4), span_of(j->prompt_len, W * 4),
+                       span_of(j->drafted, N * 4), span_of(j->repetition, W * 4), span_of(j->presence, W * 4),
+                       span_of(j->frequency, W * 4), span_of(j->bias_start, (W + 1) * 8), span_of(j->bias_ids, j->bias_len * 4),
+                       span_of(j->bias_values, j->bias_len * 4),
+                       span_of(j->allowed, j->allowed ? ((j->mask_rows - 1) * j->allowed_stride + (V + 31) / 32) * 4 : 0),
+                       span_of(j->allowed_row, N * 4)};
+    const Span rows = span_of(logits, ((N - 1) * params->row_stride + V) * elt);
+    for (const Span& x : o)
+        for (const Span& y : in)
+            if (meet(x, y)) return fail(CIAR_EINVAL, "an output overlaps an input");
+    if (meet(o[1], rows) || meet(o[0], o[1])) return fail(CIAR_EINVAL, "left overlaps the logits or out");
+    if (meet(o[0], rows) && (out != logits || out_stride != params->row_stride))
+        return fail(CIAR_EINVAL, "out overlaps logits without being them");
+    if (left) {
+        const size_t need = ciar_adjust_workspace_bytes(N, params);
+        if (!workspace) return fail(CIAR_EWORKSPACE, "workspace is NULL but %zu bytes are needed", need);
+        if (!aligned(workspace, 16)) return fail(CIAR_EALIGN, "workspace is not 16-byte aligned");
+        if (workspace_bytes < need) return fail(CIAR_EWORKSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, need);
+    }
+    ciar::LogitArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.logits = logits; a.out = out; a.N = N; a.stride = params->row_stride; a.out_stride = out_stride;
+    a.V = params->vocab; a.window = params->window; a.left = left;
+    a.left_words = left ? static_cast<uint64_t*>(workspace) : nullptr;
+    a.tag = ciar::next_tag();
+    a.history_start = j->history_start; a.history = j->history; a.history_len = j->history_len; a.prompt_len = j->prompt_len;
+    a.drafted = j->drafted; a.repetition = j->repetition; a.presence = j->presence; a.frequency = j->frequency;
+    a.bias_start = j->bias_start; a.bias_ids = j->bias_ids; a.bias_values = j->bias_values; a.bias_len = j->bias_len;
+    a.allowed = j->allowed; a.allowed_row = j->allowed_row; a.allowed_stride = j->allowed_stride; a.mask_rows = j->mask_rows;
+    ciar::discard_stale_hip_error();
+    const hipError_t e = ciar::launch_adjust(params->dtype, a, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return hip_fail(e, "logit kernel launch");
+    return CIAR_OK;
+}
+
+}  // extern "C"

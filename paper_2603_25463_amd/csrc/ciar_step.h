@@ -1,0 +1,80 @@
+// Internal interface between the C ABI (ciar_step.cpp) and the kernels of the verification step around the accept test:
+// cache plan, rotary positions, attention over the paged cache, the logits' adjustments.  Public contract: include/ciar.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ciar {
+
+constexpr int kAtom = 16;              // tokens of one head that lie together in the cache
+
+// All pointers are device pointers, as in include/ciar.h.
+struct PlanArgs {
+    const int32_t *lengths, *kept, *fresh, *held;      // [R]; kept may be null
+    int32_t*       ring;
+    const int64_t* ring_state;
+    int32_t*       table;
+    int64_t        table_stride;
+    int32_t        R, P, width, page, T;               // P: pages of the ring
+    int32_t *out_lengths, *kv_len, *cu_new, *out_held;
+    uint8_t* granted;
+    int64_t* out_ring_state;
+    int32_t *slots, *positions, *requests;             // [T]
+};
+hipError_t launch_plan(const PlanArgs& args, hipStream_t stream);
+
+// A tensor [T, heads, D]: elements between tokens and between heads.
+struct Heads {
+    const void* p;
+    int64_t     token, head;
+};
+struct RotaryArgs {
+    Heads          q, k, v, q_out, k_out;              // (the outputs are written)
+    const int32_t* positions;
+    const double*  inv_freq;
+    void *         k_cache, *v_cache;
+    const int32_t* slots;
+    double         magnitude, sign;                    // sign of the angle
+    int64_t        slot_count;                         // slots of the cache
+    int32_t        T, q_heads, kv_heads, D, n, page;   // n: rotary_dim
+};
+hipError_t launch_rotary(int dtype, bool interleaved, const RotaryArgs& args, hipStream_t stream);
+
+struct AttentionArgs {
+    Heads          q, out;
+    const void *   k_cache, *v_cache;
+    const int32_t *table, *cu_new, *kv_len;
+    float*         lse;                                // may be null
+    int64_t        table_stride;
+    float          scale;
+    int32_t        R, T, q_heads, kv_heads, D, page, pages, width, max_new, max_len;
+};
+size_t attention_workspace(const AttentionArgs& args);
+hipError_t launch_attention(const AttentionArgs& args, void* workspace, hipStream_t stream);
+
+struct LogitArgs {
+    const void* logits;
+    void*       out;
+    int64_t     N, stride, out_stride;
+    int32_t     V, window;
+    int32_t*    left;                                  // may be null
+    uint64_t*   left_words;                            // [N] workspace, where a row's slices meet (null: no left)
+    uint32_t    tag;
+    const int64_t* history_start;                      // null: no history
+    const int32_t *history, *prompt_len, *drafted;     // prompt_len and drafted may be null
+    int64_t     history_len;
+    const float *repetition, *presence, *frequency;    // each may be null
+    const int64_t* bias_start;                         // null: no biases
+    const int32_t* bias_ids;
+    const float*   bias_values;
+    int64_t     bias_len;
+    const int32_t* allowed;                            // null: no masks
+    const int32_t* allowed_row;
+    int64_t     allowed_stride;
+    int32_t     mask_rows;
+    int32_t     slices, rows_per_wg, chunks;           // set by the launcher
+};
+hipError_t launch_adjust(int dtype, LogitArgs args, hipStream_t stream);
+
+}  // namespace ciar

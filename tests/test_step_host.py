@@ -1,0 +1,201 @@
+"""Argument checks of the verification step's operators that need no GPU: every error returns with its status before any launch.
+Pointers are fake device addresses; they are validated, never dereferenced."""
+import ctypes
+
+import pytest
+
+EINVAL, EALIGN, EWORK, EUNSUP = -1, -2, -3, -4
+FAKE = 0x7f0000000000
+GAP = 1 << 32                          # between fake tensors: far enough that none overlap
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2603_25463_amd import binding, build
+    build.build(force=False)
+    return binding.lib()
+
+
+def at(i):
+    return FAKE + i * GAP
+
+
+def _plan(L, R=4, P=64, width=8, stride=8, page=16, T=32, **over):
+    names = ["lengths", "kept", "new", "held", "ring", "ring_state", "table", "o_lengths", "kv_len", "cu_new", "o_held",
+             "granted", "o_state", "slots", "positions", "requests"]
+    p = {n: at(i) for i, n in enumerate(names)}
+    p.update(over)
+    return L.ciar_cache_plan(p["lengths"], p["kept"], p["new"], p["held"], R, p["ring"], P, p["ring_state"], p["table"], width,
+                             stride, page, T, p["o_lengths"], p["kv_len"], p["cu_new"], p["o_held"], p["granted"],
+                             p["o_state"], p["slots"], p["positions"], p["requests"], None)
+
+
+def test_plan_refusals(L):
+    from paper_2603_25463_amd.binding import last_error
+    assert _plan(L, R=-1) == EINVAL and _plan(L, T=-1) == EINVAL
+    assert _plan(L, page=24) == EUNSUP and "page_size" in last_error()
+    assert _plan(L, page=0) == EUNSUP
+    assert _plan(L, P=0) == EINVAL
+    assert _plan(L, P=1 << 27, page=32) == EUNSUP
+    assert _plan(L, width=0) == EINVAL
+    assert _plan(L, width=9) == EINVAL and "table_stride" in last_error()
+    assert _plan(L, width=1 << 28, stride=1 << 28) == EUNSUP
+    for n in ("lengths", "new", "held", "ring", "ring_state", "table", "o_lengths", "kv_len", "cu_new", "o_held", "granted",
+              "o_state", "slots", "positions", "requests"):
+        assert _plan(L, **{n: None}) == EINVAL, n
+    # outputs in place of inputs, or of each other
+    assert _plan(L, o_lengths=at(0)) == EINVAL and "overlaps" in last_error()
+    assert _plan(L, o_state=at(5)) == EINVAL
+    assert _plan(L, slots=at(14) + 4) == EINVAL
+    assert _plan(L, kv_len=at(6) + 4 * 31) == EINVAL                      # the table's last entry
+
+
+def _rotary(L, T=4, struct=None, **over):
+    from paper_2603_25463_amd.step import _RotaryParams
+    names = ["q", "k", "v", "positions", "inv_freq", "q_out", "k_out", "k_cache", "v_cache", "slots"]
+    p = {n: at(i) for i, n in enumerate(names)}
+    c = _RotaryParams(ctypes.sizeof(_RotaryParams), 1, 8, 2, 64, 64, 0, 0, 1.0, 16, 0, 10, 512, 64, 128, 64, 128, 64, 512, 64,
+                      128, 64)
+    for k, v in (struct or {}).items():
+        setattr(c, k, v)
+    p["k_out"] = None
+    p.update(over)
+    return L.ciar_rotary(p["q"], p["k"], p["v"], p["positions"], p["inv_freq"], T, ctypes.byref(c), p["q_out"], p["k_out"],
+                         p["k_cache"], p["v_cache"], p["slots"], None)
+
+
+def test_rotary_refusals(L):
+    from paper_2603_25463_amd.binding import last_error
+    dense = dict(v=None, k_cache=None, v_cache=None, slots=None, k_out=at(20))
+    assert L.ciar_rotary(at(0), at(1), None, at(3), at(4), 4, None, at(5), at(6), None, None, None, None) == EINVAL
+    for s, rc in ((dict(struct_size=8), EINVAL), (dict(reserved=1), EINVAL), (dict(dtype=2), EUNSUP), (dict(q_heads=0), EINVAL),
+                  (dict(kv_heads=-1), EINVAL), (dict(rotary_dim=3), EINVAL), (dict(rotary_dim=66), EINVAL), (dict(rotary_dim=0), EINVAL),
+                  (dict(magnitude=float("inf")), EINVAL), (dict(dtype=0), EUNSUP), (dict(head_dim=60, rotary_dim=60), EUNSUP),
+                  (dict(page_size=20), EUNSUP), (dict(cache_pages=0), EINVAL), (dict(q_stride=-1), EINVAL),
+                  (dict(q_out_stride=100), EINVAL), (dict(q_out_head_stride=32), EINVAL)):
+        assert _rotary(L, struct=s) == rc, (s, last_error())
+    assert _rotary(L, T=-1) == EINVAL
+    assert _rotary(L, k_cache=None) == EINVAL and "together" in last_error()
+    assert _rotary(L, slots=None) == EINVAL and _rotary(L, v=None) == EINVAL
+    assert _rotary(L, k_out=at(20)) == EINVAL
+    assert _rotary(L, v_cache=at(8) + 8) == EALIGN and _rotary(L, q=at(0) + 1) == EALIGN
+    assert _rotary(L, positions=None) == EINVAL and _rotary(L, inv_freq=None) == EINVAL and _rotary(L, q=None) == EINVAL
+    assert _rotary(L, q_out=at(0)) == EINVAL and "overlaps" in last_error()       # not in place
+    assert _rotary(L, v_cache=at(7)) == EINVAL
+    assert _rotary(L, q_out=at(7) + 4096) == EINVAL
+    assert _rotary(L, **{**dense, "v": at(2)}) == EINVAL
+    assert _rotary(L, **{**dense, "k_out": None}) == EINVAL
+    assert _rotary(L, **{**dense, "k_out": at(1)}) == EINVAL
+    assert _rotary(L, T=0, q=None, k=None) == 0
+
+
+def _attention(L, R=2, T=6, struct=None, ws=at(9), wsb=1 << 40, **over):
+    from paper_2603_25463_amd.step import _AttentionParams
+    names = ["q", "k_cache", "v_cache", "table", "cu_new", "kv_len", "out", "lse"]
+    p = {n: at(i) for i, n in enumerate(names)}
+    c = _AttentionParams(ctypes.sizeof(_AttentionParams), 8, 2, 64, 16, 8, 4, 100, 0.125, 0, 8, 20, 512, 64, 512, 64)
+    for k, v in (struct or {}).items():
+        setattr(c, k, v)
+    p.update(over)
+    return L.ciar_paged_attention(p["q"], p["k_cache"], p["v_cache"], p["table"], p["cu_new"], p["kv_len"], R, T,
+                                  ctypes.byref(c), p["out"], p["lse"], ws, wsb, None)
+
+
+def test_attention_refusals(L):
+    from paper_2603_25463_amd.binding import last_error
+    from paper_2603_25463_amd.step import _AttentionParams
+    for s, rc in ((dict(struct_size=8), EINVAL), (dict(reserved=1), EINVAL), (dict(q_heads=7), EINVAL), (dict(kv_heads=0), EINVAL),
+                  (dict(head_dim=80), EUNSUP), (dict(head_dim=288), EUNSUP), (dict(page_size=8), EUNSUP), (dict(cache_pages=0), EINVAL),
+                  (dict(cache_pages=1 << 28), EUNSUP), (dict(table_width=0), EINVAL), (dict(table_stride=4), EINVAL),
+                  (dict(max_new=-1), EINVAL), (dict(max_len=-1), EINVAL), (dict(scale=float("nan")), EINVAL),
+                  (dict(q_head_stride=-64), EINVAL), (dict(out_head_stride=0), EINVAL)):
+        assert _attention(L, struct=s) == rc, (s, last_error())
+    assert _attention(L, R=-1) == EINVAL and _attention(L, R=70000) == EUNSUP and _attention(L, T=1 << 30) == EUNSUP
+    for n in ("q", "k_cache", "v_cache", "table", "cu_new", "kv_len", "out"):
+        assert _attention(L, **{n: None}) == EINVAL, n
+    assert _attention(L, k_cache=at(1) + 8) == EALIGN and _attention(L, lse=at(6) + 8) == EINVAL
+    assert _attention(L, out=at(0)) == EINVAL and "overlaps" in last_error()
+    assert _attention(L, T=0, q=None, out=None) == 0
+    # a call that splits its work asks for a workspace
+    c = _AttentionParams(ctypes.sizeof(_AttentionParams), 16, 2, 128, 64, 4000, 1, 200000, 0.1, 0, 4000, 4000, 2048, 128, 2048, 128)
+    need = L.ciar_attention_workspace_bytes(1, 1, ctypes.byref(c))
+    assert need % 256 == 0
+    assert L.ciar_attention_workspace_bytes(0, 1, ctypes.byref(c)) == 0 and L.ciar_attention_workspace_bytes(1, 1, None) == 0
+    if need:
+        long = {n: getattr(c, n) for n, _ in _AttentionParams._fields_}
+        assert _attention(L, R=1, T=1, struct=long, ws=None, wsb=0) == EWORK and "needed" in last_error()
+        assert _attention(L, R=1, T=1, struct=long, wsb=need - 1024) == EWORK
+        assert _attention(L, R=1, T=1, struct=long, ws=at(9) + 8) == EALIGN
+
+
+def _adjust(L, N=16, stride=1024, out_stride=1024, ws=at(20), wsb=1 << 20, params=None, **over):
+    from paper_2603_25463_amd.binding import CiarParams
+    from paper_2603_25463_amd.step import _Adjustments
+    p = CiarParams()
+    L.ciar_params_default(ctypes.byref(p))
+    p.vocab, p.row_stride = 1000, stride
+    for k, v in (params or {}).items():
+        setattr(p, k, v)
+    a = _Adjustments(ctypes.sizeof(_Adjustments), 2, at(3), at(4), 100, at(5), at(6), at(7), at(8), at(9), at(10), at(11), at(12),
+                     10, at(13), 32, at(14))
+    outer = {"logits": at(0), "out": at(1), "left": at(2)}
+    for k, v in over.items():
+        if k in outer:
+            outer[k] = v
+        else:
+            setattr(a, k, v)
+    return L.ciar_adjust_logits(outer["logits"], N, ctypes.byref(p), ctypes.byref(a), outer["out"], out_stride, outer["left"], ws,
+                                wsb, None)
+
+
+def test_adjust_refusals(L):
+    from paper_2603_25463_amd.binding import CiarParams, last_error
+    assert _adjust(L, params=dict(struct_size=1)) == EINVAL and _adjust(L, params=dict(vocab=0)) == EINVAL
+    assert _adjust(L, params=dict(vocab=40000, row_stride=40000), out_stride=40000) == EUNSUP
+    assert _adjust(L, params=dict(window=0)) == EINVAL and _adjust(L, params=dict(dtype=3)) == EUNSUP
+    assert _adjust(L, N=-1) == EINVAL
+    assert _adjust(L, struct_size=8) == EINVAL
+    assert _adjust(L, out_stride=999) == EINVAL and _adjust(L, out_stride=1001) == EALIGN
+    assert _adjust(L, logits=None) == EINVAL and _adjust(L, out=None) == EINVAL
+    assert _adjust(L, logits=at(0) + 4) == EALIGN and _adjust(L, out=at(1) + 4) == EALIGN
+    for n in ("history", "history_start", "bias_start", "bias_ids", "bias_values", "allowed", "allowed_row"):
+        assert _adjust(L, **{n: None}) == EINVAL and "together" in last_error(), n
+    assert _adjust(L, history=None, history_start=None) == EINVAL and "prompt_len" in last_error()
+    assert _adjust(L, history_len=-1) == EINVAL and _adjust(L, bias_len=-1) == EINVAL
+    assert _adjust(L, mask_rows=0) == EINVAL and _adjust(L, allowed_stride=31) == EINVAL
+    assert _adjust(L, out=at(0) + 4096) == EINVAL and "overlaps" in last_error()
+    assert _adjust(L, out=at(0), out_stride=1028) == EINVAL                       # in place, but laid out otherwise
+    assert _adjust(L, out=at(6)) == EINVAL and _adjust(L, left=at(1) + 16) == EINVAL
+    assert _adjust(L, ws=None, wsb=0) == EWORK and _adjust(L, wsb=8) == EWORK and _adjust(L, ws=at(20) + 8) == EALIGN
+    assert _adjust(L, N=0, logits=None, out=None, ws=None, wsb=0) == 0
+    p = CiarParams()
+    assert L.ciar_adjust_workspace_bytes(0, ctypes.byref(p)) == 0 and L.ciar_adjust_workspace_bytes(100, ctypes.byref(p)) == 1024
+
+
+def test_binding_refuses_what_the_kernels_do_not_read():
+    """Types, shapes and devices are checked before the library is called (the tensors here live on the CPU)."""
+    import torch
+
+    import paper_2603_25463_amd as ciar
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    plan = dict(lengths=i32(2), new=i32(2), held=i32(2), ring=i32(8), ring_state=torch.zeros(2, dtype=torch.int64), table=i32(2, 4),
+                tokens=8, page_size=16)
+    for bad in (dict(lengths=i32(2).long()), dict(new=i32(3)), dict(ring_state=i32(2)), dict(table=i32(8)), plan):
+        with pytest.raises(ValueError):
+            ciar.cache_plan(**{**plan, **bad})
+    ks, vs = ciar.cache_shapes(4, 2, 64, 32)
+    assert ks == (4, 2, 2, 8, 16, 8) and vs == (4, 2, 2, 2, 64, 8)
+    kc, vc = torch.zeros(ks, dtype=torch.bfloat16), torch.zeros(vs, dtype=torch.bfloat16)
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16)
+    for args in ((q.float(), kc, vc), (q[..., :32], kc, vc), (q, kc.float(), vc), (q, kc, vc[:, :1]), (q, kc.transpose(0, 1), vc)):
+        with pytest.raises((TypeError, ValueError)):
+            ciar.paged_attention(*args, i32(2, 4), i32(3), i32(2), 2, 64)
+    f = torch.ones(32, dtype=torch.float64)
+    with pytest.raises(ValueError, match="layout"):
+        ciar.rotary(q, q, i32(3), f, layout="other")
+    with pytest.raises(TypeError):
+        ciar.rotary(q.half(), q.half(), i32(3), f)
+    with pytest.raises(ValueError):
+        ciar.rotary(q, q, i32(3), f)                                             # not on the GPU
+    with pytest.raises(ValueError):
+        ciar.adjust_logits(torch.zeros((2, 8)), ciar.Params())
