@@ -18,6 +18,46 @@ __device__ __forceinline__ u32x4 load16_any(const void* p)
     return v;
 }
 
+// The output's accumulators on the vector ALUs, where that is rare (a rescaling, a value that is not finite): element by element in the
+// accumulation registers.  As ordinary code such a branch would claim vector registers for all of them at once (128 of a lane's 256
+// with 64 rows of 128 to a wave, and the loop next to it would spill).  The asm hides its reads from the compiler, which would keep
+// them 19 cycles behind a matrix instruction that writes the registers, and its writes 2 before one that reads them: waited for here.
+__device__ __forceinline__ void acc_settled()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 7");
+}
+__device__ __forceinline__ void acc_written()
+{
+    asm volatile("s_nop 7");
+    __builtin_amdgcn_sched_barrier(0);
+}
+template <typename V>
+__device__ __forceinline__ void scale_acc(V& acc, float f)
+{
+    acc_settled();
+#pragma unroll
+    for (int v = 0; v < (int)(sizeof(V) / 4); ++v) {
+        float x = acc[v], t;
+        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32_e32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(f));
+        acc[v] = x;
+    }
+    acc_written();
+}
+template <typename V>
+__device__ __forceinline__ void add_acc(V& acc, const V& y, bool take)
+{
+    acc_settled();
+#pragma unroll
+    for (int v = 0; v < (int)(sizeof(V) / 4); ++v) {
+        const float z = take ? y[v] : 0.f;
+        float x = acc[v], t;
+        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_add_f32_e32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(z));
+        acc[v] = x;
+    }
+    acc_written();
+}
+
 // The new tokens of a request and what they see.
 struct Request {
     int begin, n, base, len;           // first row, rows, position of the first new token (may be negative), tokens in the cache
@@ -45,6 +85,10 @@ __device__ void fill_unclaimed(const AttentionArgs& A, int64_t from, int64_t ste
         if (d == 0 && A.lse) A.lse[t * A.q_heads + h] = -INFINITY;
     }
 }
+
+// A request's row of pages, read through the scalar cache: its loads are counted apart from those of keys and values, which
+// would otherwise all be waited for with each page.
+using table_row = const __attribute__((address_space(4))) int32_t*;
 
 // What a workgroup works on.
 struct Unit {
@@ -130,7 +174,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
     }
     const float scale = A.scale * kLog2e;
     const int64_t head_bytes = (int64_t)A.page * D * 2;
-    const int32_t* row = A.table + (int64_t)u.r * A.table_stride;
+    const table_row row = (table_row)(A.table + (int64_t)u.r * A.table_stride);
     const int atoms = (most + kAtom - 1) / kAtom;
     auto atom_at = [&](int atom) -> int64_t {                      // byte offset of an atom of the request
         const uint32_t a = (uint32_t)min(atom, atoms - 1), page = __umulhi(2 * a, P.mul) >> P.shift;
@@ -196,7 +240,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
                     ref[i] = now;
                     total[i] *= keep;
 #pragma unroll
-                    for (int b = 0; b < D / 16; ++b) acc[i][b] *= keep;
+                    for (int b = 0; b < D / 16; ++b) scale_acc(acc[i][b], keep);
                 }
                 const float sub = ref[i] == -INFINITY ? 0.f : ref[i];
                 float sum = 0.f;
@@ -239,7 +283,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
                                     if (t != 8 * grp + e) x[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
                                 const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
                                 const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), one, zero, 0, 0, 0);
-                                if (t0 + t < seen[i]) acc[i][b] += y;
+                                add_acc(acc[i][b], y, t0 + t < seen[i]);
                             }
                         }
                     }
@@ -310,6 +354,400 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
     }
 }
 
+// ---- many rows to a key head: the matrix cores' work ------------------------------------------------------------------------
+//
+// A workgroup of four waves takes 128 QT rows of one request and key head (a wave 32 QT), and a part of the tokens.  Steps of 32
+// tokens come into LDS as they lie in the cache (global_load_lds, a ring of slots, requested two or three steps ahead), and every wave
+// reads all of a step as operands of v_mfma_f32_32x32x16_bf16: a lane's 16 bytes are consecutive lanes', without conflicts.
+// With 64 rows to a wave an operand feeds two matrix instructions, and LDS is half as busy as they are (with 32, as busy).
+//
+// S^T = K Q^T: lane l holds row l % 32, and of a step's tokens the eight of each atom's half l / 32 (keys enter an atom's rows with
+// bits 2 and 3 of the token swapped, which makes a lane's accumulators consecutive tokens): they are the second product's operand
+// as they are.  A wave has its SIMD to itself, so its vector instructions have to run while its own matrix instructions do:
+// the loop's body computes the weights of step s next to the scores of step s + 1 and the output of step s - 1, all independent.  The
+// references are looked at between bodies, and a rescaling, which is rare (kSlack), waits until the output has taken step s - 1.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+using lds_ptr = __attribute__((address_space(3))) void*;
+using mem_ptr = const __attribute__((address_space(1))) void*;
+
+// `n` things in pairs over `groups`: how many each group takes.
+constexpr int pairs_of(int n, int groups) { return ((n + groups - 1) / groups + 1) / 2 * 2; }
+
+// A lane's weights of a step, as the second product takes them: eight consecutive tokens of each atom.
+template <int QT>
+struct Weights {
+    uint32_t pair[QT][8];
+    __device__ __forceinline__ bf16x8 at(int i, int atom) const
+    {
+        return __builtin_bit_cast(bf16x8, u32x4{pair[i][4 * atom], pair[i][4 * atom + 1], pair[i][4 * atom + 2], pair[i][4 * atom + 3]});
+    }
+    // (the empty asm keeps them where they are computed: they are used a step later, and would be computed there)
+    __device__ __forceinline__ void put(int i, int v, float a, float b)
+    {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        pair[i][v / 2] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+        asm volatile("" : "+v"(pair[i][v / 2]));
+    }
+};
+
+template <int D, int QT>
+__global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A, const Pages P, int blocks, int splits, int64_t work,
+                                                           float* __restrict__ part_o, float2* __restrict__ part_s)
+{
+    constexpr int KS = D / 16, DB = D / 32;                        // slices of 16 dimensions, blocks of 32
+    constexpr int ATOM = kAtom * D * 2, HALF = 2 * ATOM, SLOT = 2 * HALF;       // bytes: keys, then values of a step
+    constexpr int SLOTS = D <= 128 ? 5 : 4, AHEAD = SLOTS - 2;
+    constexpr int PIECES = HALF / 1024, MINE = (PIECES + 3) / 4;   // 1 KiB requests of a step's keys (and values), and a wave's
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    if ((int64_t)blockIdx.x >= work) {
+        fill_unclaimed(A, ((int64_t)blockIdx.x - work) * 256 + tid, ((int64_t)gridDim.x - work) * 256);
+        return;
+    }
+    Unit u;
+    {
+        int i = blockIdx.x;
+        u.h = i % A.kv_heads; i /= A.kv_heads;
+        u.split = i % splits; i /= splits;
+        u.block = blocks - 1 - i % blocks;                         // the blocks that see most come first
+        u.r = i / blocks;
+    }
+    const int g = A.q_heads / A.kv_heads;
+    const Request R = request_of(A, u.r);
+    constexpr int ROWS = 128 * QT;
+    const int rows = R.n * g, m0 = u.block * ROWS;
+    if (m0 >= rows) return;
+    const int most = min(max(R.base + min(m0 + ROWS - 1, rows - 1) / g + 1, 0), R.len);
+    const int least = min(max(R.base + m0 / g + 1, 0), R.len);
+    const int steps = (most + kSteps - 1) / kSteps, each = (steps + splits - 1) / splits;
+    const int first = u.split * each, last = min(first + each, steps);
+    if (first >= last && u.split > 0) return;
+    const int full = min(max(least / kSteps, first), last);        // steps that every row sees whole: [first, full)
+
+    bf16x8 q[QT][KS];
+    f32x16 acc[QT][DB];
+    float ref[QT], total[QT];
+    int seen[QT];
+    const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;        // (a negative scale is the queries': largest scores stay largest)
+    const float scale = fabsf(A.scale) * kLog2e;
+    const int mw = m0 + wave * 32 * QT;                            // this wave's first row
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int m = min(mw + 32 * i + col, rows - 1), j = m / g, head = u.h * g + (m - j * g);
+        seen[i] = min(max(R.base + j + 1, 0), R.len);
+        const uint16_t* qrow = static_cast<const uint16_t*>(A.q.p) + (int64_t)(R.begin + j) * A.q.token + (int64_t)head * A.q.head;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) q[i][k] = __builtin_bit_cast(bf16x8, load16_any(qrow + 16 * k + 8 * half) ^ flip);
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][b][v] = 0.f;
+        ref[i] = -INFINITY;
+        total[i] = 0.f;
+    }
+    if (first < last) {
+        const int64_t head_bytes = (int64_t)A.page * D * 2;
+        const table_row row = (table_row)(A.table + (int64_t)u.r * A.table_stride);
+        const int atoms = (most + kAtom - 1) / kAtom;
+        auto atom_at = [&](int atom) -> int64_t {
+            const uint32_t a = (uint32_t)min(atom, atoms - 1), page = __umulhi(2 * a, P.mul) >> P.shift;
+            const int p = min(max(row[page], 0), A.pages - 1);
+            return ((int64_t)p * A.kv_heads + u.h) * head_bytes + (int64_t)(a - page * P.per) * ATOM;
+        };
+        // requests of a step whose atoms lie at a0, a1
+        auto request = [&](int64_t a0, int64_t a1, int slot) {
+#pragma unroll
+            for (int x = 0; x < MINE; ++x) {
+                const int piece = min(wave + 4 * x, PIECES - 1);   // (a repeated request writes what is there)
+                const int64_t from = (piece >= PIECES / 2 ? a1 + (piece - PIECES / 2) * 1024 : a0 + piece * 1024) + lane * 16;
+                char* to = lds + slot * SLOT + piece * 1024;
+                __builtin_amdgcn_global_load_lds((mem_ptr)(static_cast<const char*>(A.k_cache) + from), (lds_ptr)to, 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((mem_ptr)(static_cast<const char*>(A.v_cache) + from), (lds_ptr)(to + HALF), 16, 0, 0);
+            }
+        };
+        const int kread = (col >> 4) * ATOM + half * 256 + ((col & 3) | (col >> 1 & 4) | (col << 1 & 8)) * 16;
+        const int vread = HALF + (half * D + col) * 16;
+        auto key = [&](int slot, int k) { return *reinterpret_cast<const bf16x8*>(lds + slot * SLOT + kread + k * 512); };
+        auto value = [&](int slot, int a, int b) { return *reinterpret_cast<const bf16x8*>(lds + slot * SLOT + vread + a * ATOM + b * 512); };
+        auto scores = [&](f32x16 (&s)[QT], int slot) {
+#pragma unroll
+            for (int i = 0; i < QT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[i][v] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const bf16x8 x = key(slot, k);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][k], s[i], 0, 0, 0);
+            }
+        };
+        auto output = [&](const Weights<QT>& w, int slot) {
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int b = 0; b < DB; ++b) {
+                    const bf16x8 x = value(slot, a, b);
+#pragma unroll
+                    for (int i = 0; i < QT; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, w.at(i, a), acc[i][b], 0, 0, 0);
+                }
+        };
+        auto largest = [&](const f32x16& s) {
+            float h = fmaxf(s[0], s[1]);
+#pragma unroll
+            for (int v = 2; v < 16; v += 2) h = fmaxf(fmaxf(s[v], s[v + 1]), h);
+            return h * scale;
+        };
+        // moves the references where scores exceed them; true if any has moved (the factors are in keep)
+        auto look = [&](const float (&high)[QT], float (&keep)[QT]) {
+            bool up = false;
+#pragma unroll
+            for (int i = 0; i < QT; ++i) up |= high[i] > ref[i] + kSlack;
+            if (!__any(up)) return false;
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+                const float now = fmaxf(ref[i], fmaxf(high[i], __shfl_xor(high[i], 32)));
+                keep[i] = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[i] - now);
+                ref[i] = now;
+                total[i] *= keep[i];
+            }
+            return true;
+        };
+        auto rescale = [&](const float (&keep)[QT]) {
+#pragma unroll
+            for (int i = 0; i < QT; ++i)
+#pragma unroll
+                for (int b = 0; b < DB; ++b) scale_acc(acc[i][b], keep[i]);
+        };
+        // the ring: step s lies in slot (s - first) % SLOTS
+        int64_t n0 = 0, n1 = 0;
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) request(atom_at(2 * (first + x)), atom_at(2 * (first + x) + 1), x);
+        n0 = atom_at(2 * (first + AHEAD));
+        n1 = atom_at(2 * (first + AHEAD) + 1);
+        int slot = 0, ahead = AHEAD % SLOTS;                       // of the step s of the body, and of the step that is requested in it
+        // What opens step s: the steps up to s + 1 (the last AHEAD - 2 requested may be under way) have arrived, and every wave is done with s - 2
+        auto open = [&](int s) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * MINE * (AHEAD - 2)) : "memory");
+            request(n0, n1, ahead);
+            ahead = ahead + 1 == SLOTS ? 0 : ahead + 1;
+            n0 = atom_at(2 * (s + AHEAD + 1));
+            n1 = atom_at(2 * (s + AHEAD + 1) + 1);
+        };
+        int s = first;
+        Weights<QT> wa, wb;
+        if (first < full) {
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * MINE * (AHEAD - 1)) : "memory");
+            f32x16 sa[QT], sb[QT];
+            float high[QT], keep[QT];
+            scores(sa, 0);
+#pragma unroll
+            for (int i = 0; i < QT; ++i) high[i] = largest(sa[i]);
+            int prev = 0;
+            // The body of step s: its weights, the scores of the next step, the output of the one before (unless it is the first).
+            // Written as groups of QT matrix instructions on one operand, each followed by its share of the vector work and by the
+            // read of the operand that the group after the next one takes; nothing moves from group to group.  Two groups of the
+            // output open the body: their operands have been there since the body before, while the next step's keys are on their way.
+            constexpr int GROUPS = KS + 2 * DB, LEAD = 2;
+            constexpr int SHARE = pairs_of(16 * QT, GROUPS), SHARE1 = pairs_of(16 * QT, KS);
+            bf16x8 op[2];                                          // operands of the next two groups
+            auto operand = [&](int n, int keys, int values) -> bf16x8 {        // of group n
+                if (n >= LEAD && n < LEAD + KS) return key(keys, n - LEAD);
+                const int o = n < LEAD ? n : n - KS;
+                return value(values, o / DB, o % DB);
+            };
+            auto body = [&](f32x16 (&now)[QT], f32x16 (&next)[QT], Weights<QT>& w, const Weights<QT>& before, auto opening) {
+                constexpr bool FIRST = decltype(opening)::value;
+                open(s);
+                const bool moved = look(high, keep);
+                const int after = slot + 1 == SLOTS ? 0 : slot + 1;
+                float sub[QT], top[QT];
+#pragma unroll
+                for (int i = 0; i < QT; ++i) {
+                    sub[i] = ref[i] == -INFINITY ? 0.f : ref[i];
+                    top[i] = -INFINITY;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) next[i][v] = 0.f;
+                }
+                if constexpr (FIRST) { op[0] = key(after, 0); op[1] = key(after, 1); }
+#pragma unroll
+                for (int n = FIRST ? LEAD : 0; n < GROUPS; ++n) {
+                    const bool keys = n >= LEAD && n < LEAD + KS;
+                    if (FIRST && !keys) {
+                        // (no step before: only the vector work)
+                    } else {
+                        const bf16x8 x = op[n & 1];
+                        const int o = n < LEAD ? n : n - KS;
+#pragma unroll
+                        for (int i = 0; i < QT; ++i) {
+                            if (keys) next[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][keys ? n - LEAD : 0], next[i], 0, 0, 0);
+                            else acc[i][keys ? 0 : o % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, before.at(i, keys ? 0 : o / DB), acc[i][keys ? 0 : o % DB], 0, 0, 0);
+                        }
+                    }
+                    // (the last two reads are the next body's first: this step's values)
+                    if (n + 2 < GROUPS) op[n & 1] = operand(n + 2, after, prev);
+                    else op[n & 1] = operand(n + 2 - GROUPS, after, slot);
+                    const int e0 = FIRST ? (n - LEAD) * SHARE1 : n * SHARE, e1 = FIRST ? e0 + SHARE1 : e0 + SHARE;
+#pragma unroll
+                    for (int e = e0; e < e1; e += 2)
+                        if (e < 16 * QT) {
+                            const int i = e / 16 < QT ? e / 16 : 0, v = e % 16;
+                            const float p0 = __builtin_amdgcn_exp2f(fmaf(now[i][v], scale, -sub[i]));
+                            const float p1 = __builtin_amdgcn_exp2f(fmaf(now[i][v + 1], scale, -sub[i]));
+                            total[i] += p0;
+                            total[i] += p1;
+                            w.put(i, v, p0, p1);
+                        }
+                    if (n >= LEAD + KS + 1) {                      // the scores are there: their largest, a piece at a time
+                        constexpr int LEFT = 2 * DB - LEAD - 1, PIECE = (16 + LEFT - 1) / (LEFT > 0 ? LEFT : 1);
+                        const int v0 = (n - LEAD - KS - 1) * PIECE;
+#pragma unroll
+                        for (int i = 0; i < QT; ++i)
+#pragma unroll
+                            for (int v = v0; v < v0 + PIECE; ++v)
+                                if (v < 16) top[i] = fmaxf(top[i], next[i][v]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (2 * DB - LEAD - 1 <= 0) {
+#pragma unroll
+                    for (int i = 0; i < QT; ++i)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) top[i] = fmaxf(top[i], next[i][v]);
+                }
+#pragma unroll
+                for (int i = 0; i < QT; ++i) high[i] = top[i] * scale;
+                if (moved) rescale(keep);
+                prev = slot;
+                slot = after;
+                ++s;
+            };
+            body(sa, sb, wa, wb, std::true_type{});
+            bool odd = true;                                       // the latest weights are in wa
+            while (s + 1 < full) {
+                body(sb, sa, wb, wa, std::false_type{});
+                body(sa, sb, wa, wb, std::false_type{});
+            }
+            if (s < full) {
+                body(sb, sa, wb, wa, std::false_type{});
+                odd = false;
+            }
+            if (odd) output(wa, prev); else output(wb, prev);
+        }
+        // the steps that rows see in part, one after another
+        for (; s < last; ++s) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            open(s);
+            const int t0 = s * kSteps;
+            if (mw < rows) {
+                f32x16 x[QT];
+                float high[QT], keep[QT];
+                scores(x, slot);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (t0 + (v >> 3) * kAtom + 8 * half + (v & 7) >= seen[i]) x[i][v] = -INFINITY;
+                    high[i] = largest(x[i]);
+                    if (scale == 0.f && high[i] != high[i]) high[i] = 0.f;
+                }
+                if (look(high, keep)) rescale(keep);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) {
+                    const float sub = ref[i] == -INFINITY ? 0.f : ref[i];
+                    float sum = 0.f;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const bool sees = t0 + (v >> 3) * kAtom + 8 * half + (v & 7) < seen[i];
+                        const float p = sees ? __builtin_amdgcn_exp2f(fmaf(x[i][v], scale, -sub)) : 0.f;
+                        sum += p;
+                        x[i][v] = p;
+                    }
+#pragma unroll
+                    for (int v = 0; v < 16; v += 2) wa.put(i, v, x[i][v], x[i][v + 1]);
+                    total[i] += sum;
+                }
+                // values that no row sees are zeros; one that is not finite must not reach the rows that do not see it (0 * inf)
+#pragma unroll 1
+                for (int a = 0; a < 2; ++a) {
+                    bf16x8 val[DB];
+                    bool bad = false;
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) {
+                        u32x4 y = __builtin_bit_cast(u32x4, value(slot, a, b));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (t0 + a * kAtom + 8 * half + e >= most) y[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) bad |= (y[e] & 0x7f80u) == 0x7f80u || (y[e] & 0x7f800000u) == 0x7f800000u;
+                        val[b] = __builtin_bit_cast(bf16x8, y);
+                    }
+                    if (!__any(bad)) {
+#pragma unroll
+                        for (int b = 0; b < DB; ++b)
+#pragma unroll
+                            for (int i = 0; i < QT; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(val[b], a ? wa.at(i, 1) : wa.at(i, 0), acc[i][b], 0, 0, 0);
+                        continue;
+                    }
+#pragma unroll 1
+                    for (int t = 0; t < kAtom && t0 + a * kAtom + t < most; ++t) {
+#pragma unroll
+                        for (int i = 0; i < QT; ++i) {
+                            bf16x8 one = a ? wa.at(i, 1) : wa.at(i, 0);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (t != 8 * half + e) one[e] = (__bf16)0.f;
+#pragma unroll
+                            for (int b = 0; b < DB; ++b) {
+                                u32x4 y = __builtin_bit_cast(u32x4, val[b]);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    if (t != 8 * half + e) y[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                                f32x16 zero;
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) zero[v] = 0.f;
+                                const f32x16 z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y), one, zero, 0, 0, 0);
+                                add_acc(acc[i][b], z, t0 + a * kAtom + t < seen[i]);
+                            }
+                        }
+                    }
+                }
+            }
+            slot = slot + 1 == SLOTS ? 0 : slot + 1;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (requests past the end: LDS is handed on when the workgroup ends)
+    }
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int m = mw + 32 * i + col;
+        const float sum = total[i] + __shfl_xor(total[i], 32);
+        if (m >= rows) continue;
+        const int j = m / g, head = u.h * g + (m - j * g);
+        const int64_t t = R.begin + j;
+        if (splits == 1) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            char* o = (char*)A.out.p + (t * A.out.token + (int64_t)head * A.out.head) * 2;
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; v += 4) {
+                    bf16x4 y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = (__bf16)(acc[i][b][v + e] * inv);
+                    __builtin_memcpy(o + (32 * b + 2 * v + 4 * half) * 2, &y, 8);
+                }
+            if (half == 0 && A.lse) A.lse[t * A.q_heads + head] = sum == 0.f ? -INFINITY : (ref[i] + __builtin_amdgcn_logf(sum)) * kLn2f;
+        } else {
+            const int64_t at = ((int64_t)u.split * A.T + t) * A.q_heads + head;
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; v += 4)
+                    *reinterpret_cast<f32x4*>(part_o + at * D + 32 * b + 2 * v + 4 * half) = f32x4{acc[i][b][v], acc[i][b][v + 1], acc[i][b][v + 2], acc[i][b][v + 3]};
+            if (half == 0) part_s[at] = {ref[i], sum};
+        }
+    }
+}
+
 // The parts' rows meet: one workgroup per row; D / 4 threads to a part.
 template <int D>
 __global__ __launch_bounds__(256) void join_kernel(const AttentionArgs A, int blocks, int rows_per_block, int splits,
@@ -367,20 +805,22 @@ __global__ __launch_bounds__(256) void join_kernel(const AttentionArgs A, int bl
     if (tid == 0 && A.lse) A.lse[at] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2f;
 }
 
-// How a call is laid out: rows of a workgroup (16 rt), blocks of rows per request and key head, parts of the tokens.
+// How a call is laid out: rows of a workgroup, blocks of rows per request and key head, parts of the tokens.
 struct Shape {
-    int rt, blocks, splits;
+    bool many;
+    int rows, blocks, splits;
 };
 Shape shape_of(const AttentionArgs& a)
 {
     Shape s;
     const int64_t rows = (int64_t)a.max_new * (a.q_heads / a.kv_heads);
-    const int widest = a.D <= 128 ? 4 : a.D <= 256 ? 2 : 1;
-    s.rt = rows <= 16 ? 1 : rows <= 32 || widest == 2 ? 2 : 4;
-    s.blocks = (int)((rows + 16 * s.rt - 1) / (16 * s.rt));
+    s.many = rows > 64;
+    if (s.many) s.rows = a.D <= 128 && rows > 128 ? 256 : 128;
+    else s.rows = rows <= 16 ? 16 : rows <= 32 || a.D > 128 ? 32 : 64;
+    s.blocks = (int)((rows + s.rows - 1) / s.rows);
     if (s.blocks < 1) s.blocks = 1;
     const int64_t units = (int64_t)a.R * a.kv_heads * s.blocks;
-    const int64_t wanted = 1024, longest = (a.max_len + 255) / 256;
+    const int64_t wanted = s.many ? 512 : 1024, longest = (a.max_len + 255) / 256;
     int64_t n = units > 0 ? (wanted + units - 1) / units : 1;
     if (n > longest) n = longest;
     if (n > 256) n = 256;
@@ -388,28 +828,45 @@ Shape shape_of(const AttentionArgs& a)
     return s;
 }
 
+// Asks once per device for the dynamic LDS that a kernel needs.
+hipError_t allow_lds(const void* kernel, int bytes)
+{
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+template <int D, int QT>
+hipError_t launch_many(const AttentionArgs& a, const Shape& s, unsigned grid, int64_t work, float* po, float2* ps, hipStream_t stream)
+{
+    constexpr int bytes = (D <= 128 ? 5 : 4) * 4 * kAtom * D * 2;
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&many_rows_kernel<D, QT>), bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((many_rows_kernel<D, QT>), dim3(grid), dim3(256), bytes, stream, a, pages_of(a.page), s.blocks, s.splits, work, po, ps);
+    return hipGetLastError();
+}
+
 template <int D>
-hipError_t launch_few(const AttentionArgs& a, const Shape& s, void* workspace, hipStream_t stream)
+hipError_t launch_shape(const AttentionArgs& a, const Shape& s, void* workspace, hipStream_t stream)
 {
     const int64_t work = (int64_t)a.R * a.kv_heads * s.blocks * s.splits, grid = work + 32;
-    if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const int64_t join = (int64_t)a.R * a.kv_heads * s.blocks * s.rows;
+    if (grid > 0x7fffffffLL || join > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const int64_t rows = (int64_t)s.splits * a.T * a.q_heads;
     float* po = static_cast<float*>(workspace);
     float2* ps = s.splits > 1 ? reinterpret_cast<float2*>(po + rows * D) : nullptr;
-    const Pages P = pages_of(a.page);
     const dim3 g((unsigned)grid), b(256);
-    switch (s.rt) {
-        case 1: hipLaunchKernelGGL((few_rows_kernel<D, 1>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps); break;
-        case 2: hipLaunchKernelGGL((few_rows_kernel<D, 2>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps); break;
-        default:
-            if constexpr (D <= 128) hipLaunchKernelGGL((few_rows_kernel<D, 4>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
-            else return hipErrorInvalidValue;
+    hipError_t e;
+    if (s.many) {
+        if constexpr (D <= 128) e = s.rows == 256 ? launch_many<D, 2>(a, s, (unsigned)grid, work, po, ps, stream) : launch_many<D, 1>(a, s, (unsigned)grid, work, po, ps, stream);
+        else e = launch_many<D, 1>(a, s, (unsigned)grid, work, po, ps, stream);
+    } else {
+        const Pages P = pages_of(a.page);
+        if (s.rows == 16) hipLaunchKernelGGL((few_rows_kernel<D, 1>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
+        else if (s.rows == 32) hipLaunchKernelGGL((few_rows_kernel<D, 2>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
+        else if constexpr (D <= 128) hipLaunchKernelGGL((few_rows_kernel<D, 4>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
+        e = hipGetLastError();
     }
-    hipError_t e = hipGetLastError();
     if (e != hipSuccess || s.splits == 1) return e;
-    const int64_t join = (int64_t)a.R * a.kv_heads * s.blocks * 16 * s.rt;
-    if (join > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)join), b, 0, stream, a, s.blocks, 16 * s.rt, s.splits, po, ps);
+    hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, po, ps);
     return hipGetLastError();
 }
 
@@ -426,14 +883,14 @@ hipError_t launch_attention(const AttentionArgs& args, void* workspace, hipStrea
     if (args.T <= 0) return hipSuccess;
     const Shape s = shape_of(args);
     switch (args.D) {
-        case 32: return launch_few<32>(args, s, workspace, stream);
-        case 64: return launch_few<64>(args, s, workspace, stream);
-        case 96: return launch_few<96>(args, s, workspace, stream);
-        case 128: return launch_few<128>(args, s, workspace, stream);
-        case 160: return launch_few<160>(args, s, workspace, stream);
-        case 192: return launch_few<192>(args, s, workspace, stream);
-        case 224: return launch_few<224>(args, s, workspace, stream);
-        case 256: return launch_few<256>(args, s, workspace, stream);
+        case 32: return launch_shape<32>(args, s, workspace, stream);
+        case 64: return launch_shape<64>(args, s, workspace, stream);
+        case 96: return launch_shape<96>(args, s, workspace, stream);
+        case 128: return launch_shape<128>(args, s, workspace, stream);
+        case 160: return launch_shape<160>(args, s, workspace, stream);
+        case 192: return launch_shape<192>(args, s, workspace, stream);
+        case 224: return launch_shape<224>(args, s, workspace, stream);
+        case 256: return launch_shape<256>(args, s, workspace, stream);
         default: return hipErrorInvalidValue;
     }
 }
