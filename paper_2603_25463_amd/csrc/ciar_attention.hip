@@ -18,36 +18,33 @@ __device__ __forceinline__ u32x4 load16_any(const void* p)
     return v;
 }
 
-// The output's accumulators on the vector ALUs, where that is rare (a rescaling, a value that is not finite): element by element in the
-// accumulation registers.  As ordinary code such a branch would claim vector registers for all of them at once (128 of a lane's 256
-// with 64 rows of 128 to a wave, and the loop next to it would spill).  The asm hides its reads from the compiler, which would keep
-// them 19 cycles behind a matrix instruction that writes the registers, and its writes 2 before one that reads them: waited for here.
-__device__ __forceinline__ void acc_settled()
+// Queries: only matrix instructions read them, from accumulation registers as well as from vector registers, which are short.
+__device__ __forceinline__ bf16x8 in_acc(u32x4 v)
 {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_nop 15\n\ts_nop 7");
+    asm volatile("" : "+a"(v));
+    return __builtin_bit_cast(bf16x8, v);
 }
-__device__ __forceinline__ void acc_written()
+
+// The scale of the scores in binary orders, positive: a negative scale's sign goes to the queries (largest scores stay largest), and
+// with a scale of zero the queries are zeros (a hidden score, -inf, stays that).
+struct Scale {
+    float scale;
+    uint32_t keep, flip;
+};
+__device__ __forceinline__ Scale scale_of(float scale)
 {
-    asm volatile("s_nop 7");
-    __builtin_amdgcn_sched_barrier(0);
+    return {scale == 0.f ? 1.f : fabsf(scale) * kLog2e, scale == 0.f ? 0u : ~0u, scale < 0.f ? 0x80008000u : 0u};
 }
-template <typename V>
-__device__ __forceinline__ void scale_acc(V& acc, float f)
-{
-    acc_settled();
-#pragma unroll
-    for (int v = 0; v < (int)(sizeof(V) / 4); ++v) {
-        float x = acc[v], t;
-        asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32_e32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(f));
-        acc[v] = x;
-    }
-    acc_written();
-}
+
+// Adds y to accumulators where `take`, element by element in the accumulation registers (a value that is not finite: rare).  As ordinary
+// code such a branch would claim vector registers for all of a lane's accumulators at once.  The asm hides its reads from the
+// compiler, which would keep them 19 cycles behind a matrix instruction that writes the registers, and its writes 2 before one that
+// reads them: waited for here.
 template <typename V>
 __device__ __forceinline__ void add_acc(V& acc, const V& y, bool take)
 {
-    acc_settled();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 7");
 #pragma unroll
     for (int v = 0; v < (int)(sizeof(V) / 4); ++v) {
         const float z = take ? y[v] : 0.f;
@@ -55,7 +52,28 @@ __device__ __forceinline__ void add_acc(V& acc, const V& y, bool take)
         asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_add_f32_e32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(z));
         acc[v] = x;
     }
-    acc_written();
+    asm volatile("s_nop 7");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ bool not_finite(u32x4 v)                 // any of eight bfloat16 values
+{
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+}
+// Eight consecutive tokens' values of one dimension, the first of them token `t`: those from `end` on as zeros, and of the others
+// the finite ones (the rest as zeros), or with `other` the rest (and zeros).
+__device__ __forceinline__ u32x4 cleaned(u32x4 v, int t, int end, bool other)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t part = e & 1 ? 0xffff0000u : 0x0000ffffu, top = e & 1 ? 0x7f800000u : 0x7f80u;
+        const bool finite = (v[e / 2] & top) != top;
+        if (t + e >= end || finite == other) v[e / 2] &= ~part;
+    }
+    return v;
 }
 
 // The new tokens of a request and what they see.
@@ -111,7 +129,13 @@ Pages pages_of(int page)
 }
 
 constexpr int kSteps = 32;             // tokens of a step: two atoms
-constexpr float kSlack = 8.f;          // binary orders that a row's weights may grow beyond the reference before it is moved
+
+// The reference of a softmax (its weights are 2^(s - reference)) stands still: it is the largest score of the first step that a wave takes,
+// which most rows' later scores do not exceed by much, and weights of up to 2^kSlack lose nothing in 32 bits or bfloat16.  The largest score
+// is followed, and a wave that finds it further up, or an output out of range, takes its steps once more, with the largest itself.
+// (Moving the reference step by step costs a maximum over a row's lanes and a branch around a rescaling of the accumulators each
+// time, and with the branch registers for two copies of them.)
+constexpr float kSlack = 32.f;
 
 // ---- few rows to a key head: the cache streams by once ----------------------------------------------------------------------
 //
@@ -119,13 +143,13 @@ constexpr float kSlack = 8.f;          // binary orders that a row's weights may
 // side by side) of one request and key head, and a part of its tokens.  The waves deal the part's steps of 32 tokens among
 // themselves, each with all the rows and a softmax of its own; keys and values go from memory into the registers that the matrix
 // instructions take them from (the cache is laid out for that), requested a step ahead, through no LDS and past no barrier: what
-// bounds this kernel is memory.  At the end the waves' rows meet in LDS.
+// bounds this kernel is memory.  At the end the waves' rows meet in LDS.  Keys and values are read once in a call and pass the caches
+// by (non-temporal): one token of 64 requests over 4096 149 -> 140 us, windows over 4100 58.4 -> 54.6, one token over 200001 46.7 -> 42.7
+// (inputs that change from call to call; the same 200 MB again and again come from the memory-side cache, 32 us against 50).
 //
-// Scores as S^T = K Q^T: a lane's accumulators belong to one row (l % 16), so that reference, sum and the rescaling of the output
-// stay in the lane.  Two products of 16 tokens make a step, their tokens chosen so that a lane's eight weights are eight
-// consecutive tokens, as the second product (O^T = V^T P^T) wants them: the first takes tokens 8 g .. 8 g + 3 of the step as its rows
-// 4 g ..., the second 8 g + 4 ....  The reference of a row moves only where a score exceeds it by more than kSlack: a vote of
-// the wave, where a maximum over the row's four lanes and a rescaling of the output would be made each time.
+// Scores as S^T = K Q^T: a lane's accumulators belong to one row (l % 16), so that reference and sum stay in the lane.  Two products
+// of 16 tokens make a step, their tokens chosen so that a lane's eight weights are eight consecutive tokens, as the second product
+// (O^T = V^T P^T) wants them: the first takes tokens 8 g .. 8 g + 3 of the step as its rows 4 g ..., the second 8 g + 4 ....
 template <int D, int RT>
 __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, const Pages P, int blocks, int splits, int64_t work,
                                                        float* __restrict__ part_o, float2* __restrict__ part_s)
@@ -157,6 +181,8 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
     if (first >= last && u.split > 0) return;                      // (a row that sees nothing is the first part's)
 
     bf16x8 q[RT][D / 32];
+    const Scale scaled = scale_of(A.scale);
+    const float scale = scaled.scale;
     f32x4 acc[RT][D / 16];
     float ref[RT], total[RT];
     int seen[RT];
@@ -166,13 +192,12 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
         seen[i] = min(max(R.base + j + 1, 0), R.len);
         const uint16_t* qrow = static_cast<const uint16_t*>(A.q.p) + (int64_t)(R.begin + j) * A.q.token + (int64_t)head * A.q.head;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) q[i][k] = __builtin_bit_cast(bf16x8, load16_any(qrow + 32 * k + 8 * grp));
+        for (int k = 0; k < D / 32; ++k) q[i][k] = in_acc((load16_any(qrow + 32 * k + 8 * grp) & scaled.keep) ^ scaled.flip);
 #pragma unroll
         for (int b = 0; b < D / 16; ++b) acc[i][b] = {0.f, 0.f, 0.f, 0.f};
         ref[i] = -INFINITY;
         total[i] = 0.f;
     }
-    const float scale = A.scale * kLog2e;
     const int64_t head_bytes = (int64_t)A.page * D * 2;
     const table_row row = (table_row)(A.table + (int64_t)u.r * A.table_stride);
     const int atoms = (most + kAtom - 1) / kAtom;
@@ -188,114 +213,159 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
         const char* p = static_cast<const char*>(A.k_cache) + (col < 8 ? a0 : a1) + koff;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
-            k0[k] = *reinterpret_cast<const bf16x8*>(p + k * 1024);
-            k1[k] = *reinterpret_cast<const bf16x8*>(p + k * 1024 + 64);
+            k0[k] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p + k * 1024));
+            k1[k] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p + k * 1024 + 64));
         }
     };
     auto load_values = [&](int64_t a0, int64_t a1) {
         const char* p = static_cast<const char*>(A.v_cache) + (grp < 2 ? a0 : a1) + voff;
 #pragma unroll
-        for (int b = 0; b < D / 16; ++b) v[b] = *reinterpret_cast<const bf16x8*>(p + b * 256);
+        for (int b = 0; b < D / 16; ++b) v[b] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p + b * 256));
     };
+    float s[RT][8];
+    auto scores = [&]() {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0[k], q[i][k], s0, 0, 0, 0);
+                s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1[k], q[i][k], s1, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[i][e] = e < 4 ? s0[e & 3] : s1[e & 3];
+        }
+    };
+    auto hide = [&](int t0) {                                      // tokens that a row does not see
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (t0 + 8 * grp + e >= seen[i]) s[i][e] = -INFINITY;
+    };
+    auto largest = [&](int i) {
+        return fmaxf(fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])), fmaxf(fmaxf(s[i][4], s[i][5]), fmaxf(s[i][6], s[i][7]))) * scale;
+    };
+    auto weights = [&](int i, bf16x8& w) -> float {
+        const float sub = ref[i] == -INFINITY ? 0.f : ref[i];
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[i][e], scale, -sub));
+            sum += p;
+            w[e] = (__bf16)p;
+        }
+        return sum;
+    };
+    bool odd = false;                                              // a value that some rows must not see is not finite
     if (first + wave < last) {
-        int step = first + wave;
-        int64_t a0 = atom_at(2 * step), a1 = atom_at(2 * step + 1);
-        load_keys(a0, a1);
-        load_values(a0, a1);
-        int64_t n0 = atom_at(2 * (step + 4)), n1 = atom_at(2 * (step + 4) + 1);
-        for (; step < last; step += 4) {
-            const int t0 = step * kSteps;
-            f32x4 s0[RT], s1[RT];
-#pragma unroll
-            for (int i = 0; i < RT; ++i) s0[i] = s1[i] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k)
-#pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    s0[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0[k], q[i][k], s0[i], 0, 0, 0);
-                    s1[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1[k], q[i][k], s1[i], 0, 0, 0);
-                }
-            // the next step's keys, into the registers that have just been read (past the part's end: the last atom's again)
-            a0 = n0; a1 = n1;
-            load_keys(a0, a1);
-            n0 = atom_at(2 * (step + 8)); n1 = atom_at(2 * (step + 8) + 1);
-            const bool edge = t0 + kSteps > least;
-            bf16x8 w[RT];
+        for (int pass = 0;; ++pass) {
+            float high[RT];
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                float s[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[e] = (e < 4 ? s0[i][e & 3] : s1[i][e & 3]) * scale;
-                if (edge) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (t0 + 8 * grp + e >= seen[i]) s[e] = -INFINITY;
-                }
-                float high = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-                if (__any(high > ref[i] + kSlack)) {
-                    high = fmaxf(high, __shfl_xor(high, 16));
-                    high = fmaxf(high, __shfl_xor(high, 32));
-                    const float now = fmaxf(ref[i], high);
-                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[i] - now);
-                    ref[i] = now;
-                    total[i] *= keep;
-#pragma unroll
-                    for (int b = 0; b < D / 16; ++b) scale_acc(acc[i][b], keep);
-                }
-                const float sub = ref[i] == -INFINITY ? 0.f : ref[i];
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(s[e] - sub);
-                    sum += p;
-                    w[i][e] = (__bf16)p;
-                }
-                total[i] += sum;                                   // (of this lane's tokens; the row's lanes meet at the end)
+                for (int b = 0; b < D / 16; ++b) acc[i][b] = {0.f, 0.f, 0.f, 0.f};
+                total[i] = 0.f;
+                high[i] = -INFINITY;
             }
-            if (edge) {
-                // Where rows see different tokens, a value that is no number must not reach the rows that do not see it (0 * inf).
-                // Values that no row sees are taken as zeros; if one is left that is not finite, the tokens go in one by one.
-                bool bad = false;
-#pragma unroll
-                for (int b = 0; b < D / 16; ++b) {
-                    u32x4 x = __builtin_bit_cast(u32x4, v[b]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (t0 + 8 * grp + e >= most) x[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
-                    v[b] = __builtin_bit_cast(bf16x8, x);
-                }
-                if (__any(bad)) {
-#pragma unroll 1
-                    for (int t = 0; t < kSteps && t0 + t < most; ++t) {
-#pragma unroll
-                        for (int i = 0; i < RT; ++i) {
-                            bf16x8 one = w[i];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (t != 8 * grp + e) one[e] = (__bf16)0.f;
-#pragma unroll
-                            for (int b = 0; b < D / 16; ++b) {
-                                u32x4 x = __builtin_bit_cast(u32x4, v[b]);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (t != 8 * grp + e) x[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
-                                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-                                const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), one, zero, 0, 0, 0);
-                                add_acc(acc[i][b], y, t0 + t < seen[i]);
-                            }
-                        }
-                    }
-                    load_values(a0, a1);
-                    continue;
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < D / 16; ++b)
-#pragma unroll
-                for (int i = 0; i < RT; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[b], w[i], acc[i][b], 0, 0, 0);
+            int step = first + wave;
+            int64_t a0 = atom_at(2 * step), a1 = atom_at(2 * step + 1);
+            load_keys(a0, a1);
             load_values(a0, a1);
+            int64_t n0 = atom_at(2 * (step + 4)), n1 = atom_at(2 * (step + 4) + 1);
+            if (pass == 0) {
+                scores();
+                if ((step + 1) * kSteps > least) hide(step * kSteps);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    float h = largest(i);
+                    h = fmaxf(h, __shfl_xor(h, 16));
+                    ref[i] = fmaxf(fmaxf(h, __shfl_xor(h, 32)), -INFINITY);
+                }
+            }
+            for (; step < last; step += 4) {
+                const int t0 = step * kSteps;
+                scores();
+                // the next step's keys, into the registers that have just been read (past the part's end: the last atom's again)
+                a0 = n0; a1 = n1;
+                load_keys(a0, a1);
+                n0 = atom_at(2 * (step + 8)); n1 = atom_at(2 * (step + 8) + 1);
+                if (t0 + kSteps > least) {
+                    // Where rows see different tokens, a value that is not finite must not reach those that do not see it (0 * inf):
+                    // it is left out here.
+                    hide(t0);
+#pragma unroll
+                    for (int b = 0; b < D / 16; ++b) {
+                        const u32x4 x = __builtin_bit_cast(u32x4, v[b]);
+                        const u32x4 y = cleaned(x, t0 + 8 * grp, most, false);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) odd |= t0 + 8 * grp + e < most && (x[e / 2] ^ y[e / 2]) & (e & 1 ? 0xffff0000u : 0xffffu);
+                        v[b] = __builtin_bit_cast(bf16x8, y);
+                    }
+                }
+                bf16x8 w[RT];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    high[i] = fmaxf(high[i], largest(i));
+                    total[i] += weights(i, w[i]);                  // (of this lane's tokens; the row's lanes meet at the end)
+                }
+#pragma unroll
+                for (int b = 0; b < D / 16; ++b)
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[b], w[i], acc[i][b], 0, 0, 0);
+                load_values(a0, a1);
+            }
+            if (pass == 1) break;
+            bool again = false;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                bool wide = false;
+#pragma unroll
+                for (int b = 0; b < D / 16; ++b)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) wide |= !(fabsf(acc[i][b][x]) < INFINITY);
+                again |= high[i] > ref[i] + kSlack || (wide && high[i] > ref[i]);
+            }
+            if (!__any(again)) break;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const float h = fmaxf(high[i], __shfl_xor(high[i], 16));
+                ref[i] = fmaxf(ref[i], fmaxf(h, __shfl_xor(h, 32)));
+            }
+        }
+    }
+    if (__any(odd)) {
+        // What was left out: token by token, to the rows that see it (and make no number, or an infinity, of them).
+#pragma unroll 1
+        for (int step = first + wave; step < last; step += 4) {
+            const int t0 = step * kSteps;
+            if (t0 + kSteps <= least) continue;
+            const int64_t a0 = atom_at(2 * step), a1 = atom_at(2 * step + 1);
+            load_keys(a0, a1);
+            load_values(a0, a1);
+            scores();
+            hide(t0);
+#pragma unroll 1
+            for (int t = 0; t < kSteps && t0 + t < most; ++t) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    bf16x8 w;
+                    (void)weights(i, w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (t != 8 * grp + e) w[e] = (__bf16)0.f;
+#pragma unroll
+                    for (int b = 0; b < D / 16; ++b) {
+                        u32x4 x = cleaned(__builtin_bit_cast(u32x4, v[b]), t0 + 8 * grp, most, true);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (t != 8 * grp + e) x[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                        const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), w, zero, 0, 0, 0);
+                        add_acc(acc[i][b], y, t0 + t < seen[i]);
+                    }
+                }
+            }
         }
     }
     // the waves' rows meet, sixteen at a time
@@ -364,8 +434,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
 // S^T = K Q^T: lane l holds row l % 32, and of a step's tokens the eight of each atom's half l / 32 (keys enter an atom's rows with
 // bits 2 and 3 of the token swapped, which makes a lane's accumulators consecutive tokens): they are the second product's operand
 // as they are.  A wave has its SIMD to itself, so its vector instructions have to run while its own matrix instructions do:
-// the loop's body computes the weights of step s next to the scores of step s + 1 and the output of step s - 1, all independent.  The
-// references are looked at between bodies, and a rescaling, which is rare (kSlack), waits until the output has taken step s - 1.
+// the loop's body computes the weights of step s next to the scores of step s + 1 and the output of step s - 1, all independent.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 using lds_ptr = __attribute__((address_space(3))) void*;
 using mem_ptr = const __attribute__((address_space(1))) void*;
@@ -428,8 +497,8 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
     f32x16 acc[QT][DB];
     float ref[QT], total[QT];
     int seen[QT];
-    const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;        // (a negative scale is the queries': largest scores stay largest)
-    const float scale = fabsf(A.scale) * kLog2e;
+    const Scale scaled = scale_of(A.scale);
+    const float scale = scaled.scale;
     const int mw = m0 + wave * 32 * QT;                            // this wave's first row
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
@@ -437,15 +506,22 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
         seen[i] = min(max(R.base + j + 1, 0), R.len);
         const uint16_t* qrow = static_cast<const uint16_t*>(A.q.p) + (int64_t)(R.begin + j) * A.q.token + (int64_t)head * A.q.head;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) q[i][k] = __builtin_bit_cast(bf16x8, load16_any(qrow + 16 * k + 8 * half) ^ flip);
-#pragma unroll
-        for (int b = 0; b < DB; ++b)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][b][v] = 0.f;
+        for (int k = 0; k < KS; ++k) q[i][k] = in_acc((load16_any(qrow + 16 * k + 8 * half) & scaled.keep) ^ scaled.flip);
         ref[i] = -INFINITY;
-        total[i] = 0.f;
     }
-    if (first < last) {
+    bool odd = false;                                              // a value that some rows must not see is not finite
+    for (int pass = 0;; ++pass) {
+        float high[QT];                                            // largest score so far
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][b][v] = 0.f;
+            total[i] = 0.f;
+            high[i] = -INFINITY;
+        }
+        if (first >= last) break;
         const int64_t head_bytes = (int64_t)A.page * D * 2;
         const table_row row = (table_row)(A.table + (int64_t)u.r * A.table_stride);
         const int atoms = (most + kAtom - 1) / kAtom;
@@ -497,27 +573,14 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
             for (int v = 2; v < 16; v += 2) h = fmaxf(fmaxf(s[v], s[v + 1]), h);
             return h * scale;
         };
-        // moves the references where scores exceed them; true if any has moved (the factors are in keep)
-        auto look = [&](const float (&high)[QT], float (&keep)[QT]) {
-            bool up = false;
-#pragma unroll
-            for (int i = 0; i < QT; ++i) up |= high[i] > ref[i] + kSlack;
-            if (!__any(up)) return false;
+        auto refer = [&](const f32x16 (&s)[QT]) {                  // references from a first step's scores
 #pragma unroll
             for (int i = 0; i < QT; ++i) {
-                const float now = fmaxf(ref[i], fmaxf(high[i], __shfl_xor(high[i], 32)));
-                keep[i] = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[i] - now);
-                ref[i] = now;
-                total[i] *= keep[i];
+                const float h = largest(s[i]);
+                ref[i] = fmaxf(fmaxf(h, __shfl_xor(h, 32)), -INFINITY);
             }
-            return true;
         };
-        auto rescale = [&](const float (&keep)[QT]) {
-#pragma unroll
-            for (int i = 0; i < QT; ++i)
-#pragma unroll
-                for (int b = 0; b < DB; ++b) scale_acc(acc[i][b], keep[i]);
-        };
+        auto hidden = [&](int t0, int i, int v) { return t0 + (v >> 3) * kAtom + 8 * half + (v & 7) >= seen[i]; };
         // the ring: step s lies in slot (s - first) % SLOTS
         int64_t n0 = 0, n1 = 0;
 #pragma unroll
@@ -538,10 +601,8 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
         if (first < full) {
             asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * MINE * (AHEAD - 1)) : "memory");
             f32x16 sa[QT], sb[QT];
-            float high[QT], keep[QT];
             scores(sa, 0);
-#pragma unroll
-            for (int i = 0; i < QT; ++i) high[i] = largest(sa[i]);
+            if (pass == 0) refer(sa);
             int prev = 0;
             // The body of step s: its weights, the scores of the next step, the output of the one before (unless it is the first).
             // Written as groups of QT matrix instructions on one operand, each followed by its share of the vector work and by the
@@ -558,13 +619,11 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
             auto body = [&](f32x16 (&now)[QT], f32x16 (&next)[QT], Weights<QT>& w, const Weights<QT>& before, auto opening) {
                 constexpr bool FIRST = decltype(opening)::value;
                 open(s);
-                const bool moved = look(high, keep);
                 const int after = slot + 1 == SLOTS ? 0 : slot + 1;
-                float sub[QT], top[QT];
+                float sub[QT];
 #pragma unroll
                 for (int i = 0; i < QT; ++i) {
                     sub[i] = ref[i] == -INFINITY ? 0.f : ref[i];
-                    top[i] = -INFINITY;
 #pragma unroll
                     for (int v = 0; v < 16; ++v) next[i][v] = 0.f;
                 }
@@ -595,28 +654,14 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
                             const float p1 = __builtin_amdgcn_exp2f(fmaf(now[i][v + 1], scale, -sub[i]));
                             total[i] += p0;
                             total[i] += p1;
+                            high[i] = fmaxf(fmaxf(now[i][v], now[i][v + 1]), high[i]);
                             w.put(i, v, p0, p1);
                         }
-                    if (n >= LEAD + KS + 1) {                      // the scores are there: their largest, a piece at a time
-                        constexpr int LEFT = 2 * DB - LEAD - 1, PIECE = (16 + LEFT - 1) / (LEFT > 0 ? LEFT : 1);
-                        const int v0 = (n - LEAD - KS - 1) * PIECE;
+                    // (sums and maxima stay in their group, too: left to itself the compiler collects them behind the body)
 #pragma unroll
-                        for (int i = 0; i < QT; ++i)
-#pragma unroll
-                            for (int v = v0; v < v0 + PIECE; ++v)
-                                if (v < 16) top[i] = fmaxf(top[i], next[i][v]);
-                    }
+                    for (int i = 0; i < QT; ++i) asm volatile("" : "+v"(total[i]), "+v"(high[i]));
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if constexpr (2 * DB - LEAD - 1 <= 0) {
-#pragma unroll
-                    for (int i = 0; i < QT; ++i)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) top[i] = fmaxf(top[i], next[i][v]);
-                }
-#pragma unroll
-                for (int i = 0; i < QT; ++i) high[i] = top[i] * scale;
-                if (moved) rescale(keep);
                 prev = slot;
                 slot = after;
                 ++s;
@@ -640,81 +685,114 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
             const int t0 = s * kSteps;
             if (mw < rows) {
                 f32x16 x[QT];
-                float high[QT], keep[QT];
                 scores(x, slot);
 #pragma unroll
-                for (int i = 0; i < QT; ++i) {
+                for (int i = 0; i < QT; ++i)
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
-                        if (t0 + (v >> 3) * kAtom + 8 * half + (v & 7) >= seen[i]) x[i][v] = -INFINITY;
-                    high[i] = largest(x[i]);
-                    if (scale == 0.f && high[i] != high[i]) high[i] = 0.f;
-                }
-                if (look(high, keep)) rescale(keep);
+                        if (hidden(t0, i, v)) x[i][v] = -INFINITY;
+                if (pass == 0 && s == first) refer(x);
 #pragma unroll
                 for (int i = 0; i < QT; ++i) {
                     const float sub = ref[i] == -INFINITY ? 0.f : ref[i];
                     float sum = 0.f;
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const bool sees = t0 + (v >> 3) * kAtom + 8 * half + (v & 7) < seen[i];
-                        const float p = sees ? __builtin_amdgcn_exp2f(fmaf(x[i][v], scale, -sub)) : 0.f;
-                        sum += p;
-                        x[i][v] = p;
-                    }
+                    for (int v = 0; v < 16; v += 2) {
+                        high[i] = fmaxf(fmaxf(x[i][v], x[i][v + 1]), high[i]);
+                        float p[2];
 #pragma unroll
-                    for (int v = 0; v < 16; v += 2) wa.put(i, v, x[i][v], x[i][v + 1]);
+                        for (int e = 0; e < 2; ++e) {
+                            p[e] = __builtin_amdgcn_exp2f(fmaf(x[i][v + e], scale, -sub));
+                            sum += p[e];
+                        }
+                        wa.put(i, v, p[0], p[1]);
+                    }
                     total[i] += sum;
                 }
-                // values that no row sees are zeros; one that is not finite must not reach the rows that do not see it (0 * inf)
-#pragma unroll 1
-                for (int a = 0; a < 2; ++a) {
-                    bf16x8 val[DB];
-                    bool bad = false;
+                // values that no row sees are zeros; one that is not finite must not reach the rows that do not see it (0 * inf): left out
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int b = 0; b < DB; ++b) {
-                        u32x4 y = __builtin_bit_cast(u32x4, value(slot, a, b));
+                        const int t = t0 + a * kAtom + 8 * half;
+                        const u32x4 y = __builtin_bit_cast(u32x4, value(slot, a, b)), z = cleaned(y, t, most, false);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (t0 + a * kAtom + 8 * half + e >= most) y[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                        for (int e = 0; e < 8; ++e) odd |= t + e < most && (y[e / 2] ^ z[e / 2]) & (e & 1 ? 0xffff0000u : 0xffffu);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) bad |= (y[e] & 0x7f80u) == 0x7f80u || (y[e] & 0x7f800000u) == 0x7f800000u;
-                        val[b] = __builtin_bit_cast(bf16x8, y);
+                        for (int i = 0; i < QT; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), wa.at(i, a), acc[i][b], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    if (!__any(bad)) {
+            }
+            slot = slot + 1 == SLOTS ? 0 : slot + 1;
+        }
+        // (requests past the end: they must not meet the next pass's, nor the workgroup that is given this LDS next)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        bool again = false;
 #pragma unroll
-                        for (int b = 0; b < DB; ++b)
+        for (int i = 0; i < QT; ++i) {
+            high[i] *= scale;
+            bool wide = false;
 #pragma unroll
-                            for (int i = 0; i < QT; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(val[b], a ? wa.at(i, 1) : wa.at(i, 0), acc[i][b], 0, 0, 0);
-                        continue;
-                    }
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) wide |= !(fabsf(acc[i][b][v]) < INFINITY);
+            again |= pass == 0 && (high[i] > ref[i] + kSlack || (wide && high[i] > ref[i]));
+        }
+        if (!__syncthreads_or(again)) {
+            if (__any(odd)) {
+                // What was left out: token by token, to the rows that see it (and make no number, or an infinity, of them).
 #pragma unroll 1
-                    for (int t = 0; t < kAtom && t0 + a * kAtom + t < most; ++t) {
+                for (s = full; s < last; ++s) {
+                    const int t0 = s * kSteps;
+#pragma unroll 1
+                    for (int a = 0; a < 2; ++a) {
+                        const char* keys = static_cast<const char*>(A.k_cache) + atom_at(2 * s + a);
+                        const char* values = static_cast<const char*>(A.v_cache) + atom_at(2 * s + a);
 #pragma unroll
                         for (int i = 0; i < QT; ++i) {
-                            bf16x8 one = a ? wa.at(i, 1) : wa.at(i, 0);
+                            f32x16 x;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (t != 8 * half + e) one[e] = (__bf16)0.f;
+                            for (int v = 0; v < 16; ++v) x[v] = 0.f;
+                            // (both halves of the product's rows are this atom's tokens: the first eight accumulators are what is wanted)
+#pragma unroll 1
+                            for (int k = 0; k < KS; ++k) {
+                                bf16x8 kk = *reinterpret_cast<const bf16x8*>(keys + (kread & (ATOM - 1)) + k * 512), qq = q[i][0];
 #pragma unroll
-                            for (int b = 0; b < DB; ++b) {
-                                u32x4 y = __builtin_bit_cast(u32x4, val[b]);
+                                for (int z = 1; z < KS; ++z)
+                                    if (k == z) qq = q[i][z];
+                                x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qq, x, 0, 0, 0);
+                            }
+                            const float sub = ref[i] == -INFINITY ? 0.f : ref[i];
+                            bf16x8 w;
+#pragma unroll
+                            for (int v = 0; v < 8; ++v) w[v] = hidden(t0 + a * kAtom, i, v) ? (__bf16)0.f : (__bf16)__builtin_amdgcn_exp2f(fmaf(x[v], scale, -sub));
+#pragma unroll 1
+                            for (int t = 0; t < kAtom && t0 + a * kAtom + t < most; ++t) {
+                                bf16x8 one = w;
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
-                                    if (t != 8 * half + e) y[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
-                                f32x16 zero;
+                                    if (t != 8 * half + e) one[e] = (__bf16)0.f;
 #pragma unroll
-                                for (int v = 0; v < 16; ++v) zero[v] = 0.f;
-                                const f32x16 z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y), one, zero, 0, 0, 0);
-                                add_acc(acc[i][b], z, t0 + a * kAtom + t < seen[i]);
+                                for (int b = 0; b < DB; ++b) {
+                                    u32x4 y = cleaned(*reinterpret_cast<const u32x4*>(values + vread - HALF + b * 512), t0 + a * kAtom + 8 * half, most, true);
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e)
+                                        if (t != 8 * half + e) y[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                                    f32x16 zero;
+#pragma unroll
+                                    for (int v = 0; v < 16; ++v) zero[v] = 0.f;
+                                    const f32x16 z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, y), one, zero, 0, 0, 0);
+                                    add_acc(acc[i][b], z, t0 + a * kAtom + t < seen[i]);
+                                }
                             }
                         }
                     }
                 }
             }
-            slot = slot + 1 == SLOTS ? 0 : slot + 1;
+            break;
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (requests past the end: LDS is handed on when the workgroup ends)
+#pragma unroll
+        for (int i = 0; i < QT; ++i) ref[i] = fmaxf(ref[i], fmaxf(high[i], __shfl_xor(high[i], 32)));
     }
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
@@ -748,61 +826,71 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
     }
 }
 
-// The parts' rows meet: one workgroup per row; D / 4 threads to a part.
-template <int D>
+// The parts' rows meet.  D / 4 threads take a row of a part; with few parts each such group takes a row and all its parts, no
+// exchange, with many (WIDE) a workgroup takes one row and its groups deal the parts among themselves.  Two rounds of loads: sums and
+// references of the group's parts, then their outputs.
+template <int D, bool WIDE>
 __global__ __launch_bounds__(256) void join_kernel(const AttentionArgs A, int blocks, int rows_per_block, int splits,
                                                    const float* __restrict__ part_o, const float2* __restrict__ part_s)
 {
-    constexpr int TPR = D / 4, AT_ONCE = 256 / TPR;
-    __shared__ f32x4 sums[AT_ONCE][TPR];
-    __shared__ float wave_top[4], wave_sum[4];
-    const int tid = threadIdx.x;
+    constexpr int TPR = D / 4, GROUPS = 256 / TPR, ROWS = WIDE ? 1 : GROUPS;
+    __shared__ f32x4 sums[WIDE ? GROUPS : 1][TPR];
+    __shared__ float2 stats[GROUPS];
+    const int tid = threadIdx.x, c = tid % TPR, group = tid / TPR;
+    const int pieces = (rows_per_block + ROWS - 1) / ROWS;
     int i = blockIdx.x;
-    const int mr = i % rows_per_block; i /= rows_per_block;
+    const int mr = (i % pieces) * ROWS + (WIDE ? 0 : group); i /= pieces;
     const int block = i % blocks; i /= blocks;
     const int h = i % A.kv_heads, r = i / A.kv_heads;
     const int g = A.q_heads / A.kv_heads;
     const Request R = request_of(A, r);
     const int rows = R.n * g, m0 = block * rows_per_block, m = m0 + mr;
-    if (m >= rows) return;
+    const bool mine = group < GROUPS && mr < rows_per_block && m < rows;
+    if (!WIDE && !mine) return;
+    if (WIDE && m >= rows) return;                                 // (the whole workgroup)
     const int most = min(max(R.base + min(m0 + rows_per_block - 1, rows - 1) / g + 1, 0), R.len);
     const int steps = (most + kSteps - 1) / kSteps, each = (steps + splits - 1) / splits;
     const int parts = each > 0 ? (steps + each - 1) / each : 1;    // those that have written
     const int j = m / g, head = h * g + (m - j * g);
     const int64_t t = R.begin + j, at = t * A.q_heads + head, step = (int64_t)A.T * A.q_heads;
-    float top = -INFINITY;
-    for (int s = tid; s < parts; s += 256) top = fmaxf(top, part_s[at + s * step].x);
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if ((tid & 63) == 0) wave_top[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
-    float sum = 0.f;
-    for (int s = tid; s < parts; s += 256) {
-        const float2 x = part_s[at + s * step];
-        sum += top == -INFINITY ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - top);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if ((tid & 63) == 0) wave_sum[tid >> 6] = sum;
+    const int s0 = WIDE ? group : 0, ds = WIDE ? GROUPS : 1;
+    float top = -INFINITY, sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    const int c = tid % TPR, s0 = tid / TPR;
-    if (s0 < AT_ONCE)
-        for (int s = s0; s < parts; s += AT_ONCE) {
-            const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part_s[at + s * step].x - top);
+    if (mine) {
+#pragma unroll 4
+        for (int s = s0; s < parts; s += ds) top = fmaxf(top, part_s[at + s * step].x);
+#pragma unroll 4
+        for (int s = s0; s < parts; s += ds) {
+            const float2 x = part_s[at + s * step];
+            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x.x - top);
+            sum += x.y * f;
             o += *reinterpret_cast<const f32x4*>(part_o + (at + s * step) * D + 4 * c) * f;
         }
-    if (s0 < AT_ONCE) sums[s0][c] = o;
-    __syncthreads();
-    if (tid >= TPR) return;
-    sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
-    o = sums[0][tid];
-    for (int s = 1; s < AT_ONCE; ++s) o += sums[s][tid];
+    }
+    if constexpr (WIDE) {
+        if (mine) {
+            sums[group][c] = o;
+            if (c == 0) stats[group] = {top, sum};
+        }
+        __syncthreads();
+        if (tid >= TPR) return;
+        const int used = min(GROUPS, parts);
+        top = -INFINITY;
+        for (int x = 0; x < used; ++x) top = fmaxf(top, stats[x].x);
+        o = {0.f, 0.f, 0.f, 0.f};
+        sum = 0.f;
+        for (int x = 0; x < used; ++x) {
+            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(stats[x].x - top);
+            sum += stats[x].y * f;
+            o += sums[x][c] * f;
+        }
+    }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    __bf16* y = (__bf16*)A.out.p + t * A.out.token + (int64_t)head * A.out.head + 4 * tid;
+    bf16x4 y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[e] * inv);
-    if (tid == 0 && A.lse) A.lse[at] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2f;
+    __builtin_memcpy((char*)A.out.p + (t * A.out.token + (int64_t)head * A.out.head + 4 * c) * 2, &y, 8);
+    if (c == 0 && A.lse) A.lse[at] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2f;
 }
 
 // How a call is laid out: rows of a workgroup, blocks of rows per request and key head, parts of the tokens.
@@ -810,21 +898,39 @@ struct Shape {
     bool many;
     int rows, blocks, splits;
 };
+constexpr int kJoinFew = 8;                                        // parts that join_kernel takes one after another
+
 Shape shape_of(const AttentionArgs& a)
 {
     Shape s;
     const int64_t rows = (int64_t)a.max_new * (a.q_heads / a.kv_heads);
-    s.many = rows > 64;
+    // (one block of few_rows_kernel: the rows whose queries and outputs a wave's registers hold)
+    s.many = rows > (a.D <= 128 ? 64 : a.D <= 192 ? 32 : 16);
     if (s.many) s.rows = a.D <= 128 && rows > 128 ? 256 : 128;
-    else s.rows = rows <= 16 ? 16 : rows <= 32 || a.D > 128 ? 32 : 64;
+    else s.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     s.blocks = (int)((rows + s.rows - 1) / s.rows);
     if (s.blocks < 1) s.blocks = 1;
+    // Parts: workgroups run in rounds of as many as the compute units hold; a part costs its steps, a start and an end, and parts cost
+    // the launch that joins them, and the writing and reading of their rows.  In us, with what the kernels measured: few rows, 0.65 us
+    // a step of four waves at 128 dimensions while memory keeps up (5.5 TB/s over all) and 5 us a workgroup; many rows, 3.4 TFLOP/s a
+    // unit and 8 us; joining, 6 us and 4 TB/s.  (Windows of 8 tokens, 32 requests, 128 units of 64 rows over 4100 tokens: 1 part 69 us, 2
+    // parts 54.6; one token, 2 units over 200001: 64 parts 56.6 us, 128 parts 42.7; one token, 512 units over 4096: 1 part 140 us, 2
+    // parts 149.)
     const int64_t units = (int64_t)a.R * a.kv_heads * s.blocks;
-    const int64_t wanted = s.many ? 512 : 1024, longest = (a.max_len + 255) / 256;
-    int64_t n = units > 0 ? (wanted + units - 1) / units : 1;
-    if (n > longest) n = longest;
-    if (n > 256) n = 256;
-    s.splits = (int)(n < 1 ? 1 : n);
+    const int per_unit = s.many ? 1 : s.rows * a.D <= 16 * 64 ? 3 : s.rows * a.D <= 16 * 128 ? 2 : 1;
+    const int64_t resident = (int64_t)compute_units() * per_unit;
+    const double step_us = s.many ? 4.0 * kSteps * s.rows * a.D / 3.4e6 : 0.65 * a.D / 128;
+    const int64_t steps = ((int64_t)a.max_len + kSteps - 1) / kSteps;
+    const double memory_us = s.many ? 0.0 : (double)units * steps * (4 * kSteps * a.D) / 5.5e6;
+    const double row_us = (double)a.T * a.q_heads * (a.D * 8 + 16) / 4e6;
+    s.splits = 1;
+    double best = 0.0;
+    for (int64_t n = 1; n <= 256 && n <= (steps + 3) / 4; n += n < 16 ? 1 : n < 64 ? 4 : 16) {
+        const int64_t rounds = (units * n + resident - 1) / resident, each = (steps + n - 1) / n;
+        const double own = (double)rounds * ((double)each * step_us + (s.many ? 8.0 : 5.0));
+        const double us = (own > memory_us + 5.0 ? own : memory_us + 5.0) + (n > 1 ? 6.0 + (double)n * row_us : 0.0);
+        if (n == 1 || us < 0.95 * best) { best = us; s.splits = (int)n; }
+    }
     return s;
 }
 
@@ -848,7 +954,9 @@ template <int D>
 hipError_t launch_shape(const AttentionArgs& a, const Shape& s, void* workspace, hipStream_t stream)
 {
     const int64_t work = (int64_t)a.R * a.kv_heads * s.blocks * s.splits, grid = work + 32;
-    const int64_t join = (int64_t)a.R * a.kv_heads * s.blocks * s.rows;
+    constexpr int at_once = 256 / (D / 4);                         // rows of a workgroup of join_kernel
+    const bool wide = s.splits > kJoinFew;
+    const int64_t join = (int64_t)a.R * a.kv_heads * s.blocks * (wide ? s.rows : (s.rows + at_once - 1) / at_once);
     if (grid > 0x7fffffffLL || join > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const int64_t rows = (int64_t)s.splits * a.T * a.q_heads;
     float* po = static_cast<float*>(workspace);
@@ -861,12 +969,14 @@ hipError_t launch_shape(const AttentionArgs& a, const Shape& s, void* workspace,
     } else {
         const Pages P = pages_of(a.page);
         if (s.rows == 16) hipLaunchKernelGGL((few_rows_kernel<D, 1>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
+        else if constexpr (D > 192) return hipErrorInvalidValue;
         else if (s.rows == 32) hipLaunchKernelGGL((few_rows_kernel<D, 2>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
         else if constexpr (D <= 128) hipLaunchKernelGGL((few_rows_kernel<D, 4>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
         e = hipGetLastError();
     }
     if (e != hipSuccess || s.splits == 1) return e;
-    hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, po, ps);
+    if (wide) hipLaunchKernelGGL((join_kernel<D, true>), dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, po, ps);
+    else hipLaunchKernelGGL((join_kernel<D, false>), dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, po, ps);
     return hipGetLastError();
 }
 

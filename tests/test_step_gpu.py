@@ -649,3 +649,25 @@ def test_step_in_a_graph(ciar):
         torch.cuda.synchronize()
         for k in want:
             assert torch.equal(got[k], want[k]), (seed, k)
+
+
+@pytest.mark.parametrize("step", [3.0, 40.0])
+@pytest.mark.parametrize("new,D", [(1, 64), (8, 128), (40, 64), (200, 128), (40, 256)])
+def test_attention_of_scores_that_climb(ciar, step, new, D):
+    """Scores that grow from token to token by far more than the range of 32 bits between the first and the last: the softmax's
+    reference is found again (values large enough to overflow where it is not)."""
+    L, Hq, Hk, page = 700, 4, 2, 16
+    kc, vc, table, kv = make_cache(ciar, [L], Hk, D, page, seed=17)
+    for i in range(L):
+        p, off = int(table[0, i // page]), i % page
+        for cache, rows, x in ((kc, kv[0][0], step * (i // 8)), (vc, kv[0][1], 1e33 if i % 2 else -2e33)):
+            rows[i, :, :] = torch.tensor(x).bfloat16().double()
+    rows_k, rows_v = kv[0]
+    i = torch.arange(L)
+    page_of, off = table[0].cpu()[i // page].long(), i % page
+    kc[page_of.cuda(), :, 0, :, off.cuda()] = rows_k.bfloat16().cuda().view(L, Hk, D // 8, 8)
+    vc[page_of.cuda(), :, 0, (off // 8).cuda(), :, (off % 8).cuda()] = rows_v.bfloat16().cuda()
+    q = torch.full((new, Hq, D), 1.0 / D).bfloat16()
+    o = ciar.paged_attention(q.cuda(), kc, vc, table, i32([0, new]), i32([L]), new, L, scale=1.0)
+    assert bool(torch.isfinite(o["out"].float()).all())
+    check_attention(o, q, kv, [new], [0], 1.0, Hq // Hk)
