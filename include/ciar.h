@@ -408,7 +408,7 @@ typedef struct ciar_rotary_params {
     uint32_t struct_size;     /* sizeof(ciar_rotary_params); checked                                        */
     int32_t  dtype;           /* ciar_dtype of q, k, v; CIAR_BF16 where a cache is given                    */
     int32_t  q_heads, kv_heads;
-    int32_t  head_dim;        /* D; a multiple of 8 where a cache is given                                  */
+    int32_t  head_dim;        /* D, at most 1024; a multiple of 8 where a cache is given                    */
     int32_t  rotary_dim;      /* the first n dimensions of a head are turned; even, 2 <= n <= D             */
     int32_t  interleaved;     /* 0: pair p is (p, p + n / 2), 1: pair p is (2 p, 2 p + 1)                   */
     int32_t  inverse;         /* 1: turned back (by -angle): the gradient of the turn                       */

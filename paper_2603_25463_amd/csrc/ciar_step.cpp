@@ -126,8 +126,7 @@ int ciar_rotary(const void* q, const void* k, const void* v, const int32_t* posi
     if (int rc = check_heads_of(p->q_heads, p->kv_heads)) return rc;
     if (p->head_dim < 2 || p->rotary_dim < 2 || p->rotary_dim > p->head_dim || p->rotary_dim % 2 != 0)
         return fail(CIAR_EINVAL, "rotary_dim %d must be even and in [2, head_dim %d]", p->rotary_dim, p->head_dim);
-    if (p->rotary_dim > 1024 || p->head_dim > 65536)
-        return fail(CIAR_EUNSUPPORTED, "rotary_dim above 1024 or head_dim above 65536 (got %d, %d)", p->rotary_dim, p->head_dim);
+    if (p->head_dim > 1024) return fail(CIAR_EUNSUPPORTED, "head_dim %d is above 1024", p->head_dim);
     if (!std::isfinite(p->magnitude)) return fail(CIAR_EINVAL, "params->magnitude is not finite");
     if (T < 0) return fail(CIAR_EINVAL, "T is negative");
     if (T > kMost) return fail(CIAR_EUNSUPPORTED, "T exceeds 2^31 - 1");
