@@ -68,23 +68,72 @@ template <> struct Row<bf16_t> {
 
 constexpr int kRotaryTokens = 16;      // most tokens of a workgroup
 
+// Heads too short for two vectors (or fewer dimensions turned than one has), or pairs side by side in heads of an odd length: one workgroup per token, one element at a time.
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rotary_short_kernel(const RotaryArgs A)
+{
+    __shared__ float2 turns[512];
+    constexpr int E = sizeof(T);
+    const int t = blockIdx.x, tid = threadIdx.x, half = A.n / 2;
+    const double pos = (double)A.positions[t] * A.sign;
+    for (int p = tid; p < half; p += 256) {
+        float c, s;
+        turn_of(pos * A.inv_freq[p], c, s);
+        turns[p] = {(float)(c * A.magnitude), (float)(s * A.magnitude)};
+    }
+    __syncthreads();
+    auto turned = [&](const char* row, int d) -> float {
+        const float x = Row<T>::load(row + (int64_t)d * E);
+        if (d >= A.n) return x;
+        const bool second = INTERLEAVED ? (d & 1) : d >= half;
+        const int p = INTERLEAVED ? d >> 1 : second ? d - half : d;
+        const int other = INTERLEAVED ? d ^ 1 : second ? d - half : d + half;
+        const float y = Row<T>::load(row + (int64_t)other * E);
+        const float2 w = turns[p];
+        return second ? x * w.x + y * w.y : x * w.x - y * w.y;
+    };
+    const int Dq = A.q_heads * A.D, Dk = A.kv_heads * A.D;
+    for (int i = tid; i < Dq; i += 256) {
+        const int h = i / A.D, d = i - h * A.D;
+        const char* row = static_cast<const char*>(A.q.p) + (t * A.q.token + h * A.q.head) * E;
+        Row<T>::store((char*)A.q_out.p + (t * A.q_out.token + h * A.q_out.head + d) * E, turned(row, d));
+    }
+    const int slot = A.k_cache ? A.slots[t] : 0;
+    if (A.k_cache && (slot < 0 || slot >= A.slot_count)) return;
+    for (int i = tid; i < Dk; i += 256) {
+        const int h = i / A.D, d = i - h * A.D;
+        const char* row = static_cast<const char*>(A.k.p) + (t * A.k.token + h * A.k.head) * E;
+        const float x = turned(row, d);
+        if (!A.k_cache) {
+            Row<T>::store((char*)A.k_out.p + (t * A.k_out.token + h * A.k_out.head + d) * E, x);
+        } else {
+            const int page = slot / A.page, off = slot - page * A.page, a = off / kAtom, at = off % kAtom;
+            const int64_t atom = (((int64_t)page * A.kv_heads + h) * (A.page / kAtom) + a) * kAtom * A.D;
+            Row<T>::store((char*)A.k_cache + (atom + (d / 8 * kAtom + at) * 8 + d % 8) * E, x);
+            const char* vrow = static_cast<const char*>(A.v.p) + (t * A.v.token + h * A.v.head) * E;
+            Row<T>::store((char*)A.v_cache + (atom + (at / 8 * A.D + d) * 8 + at % 8) * E, Row<T>::load(vrow + (int64_t)d * E));
+        }
+    }
+}
+
 // A workgroup takes up to 16 tokens and a range of their heads (queries, keys, values, in that order).  First the factors of every
 // dimension of its tokens go into LDS: y[d] = c x[d] + s x[partner of d], with c = 1, s = -0 for dimensions that are only copied (a
-// negative zero stays one).  Then every thread takes the same 16 bytes of one head row after another: its own vector, and for pairs of
-// halves the partners' (a second load of what another thread has just loaded; any offset).  Values are turned round in LDS: the cache
+// negative zero stays one).  Then every thread takes the same 16 bytes of one head row after another, four under way at once: its own
+// vector, and for pairs of halves the partners' (a second load of what another thread has just loaded; any offset; ACROSS: one of a
+// row's vectors lies across the middle of the pairs and has them at both ends).  Values are turned round in LDS: the cache
 // wants a dimension's eight tokens side by side.  Tiles begin where an atom of the cache begins if the tokens' slots are
 // consecutive (the first token's slot says where): a dimension's eight tokens are then one store; runs that are cut off are stored
 // element by element.  Bound by memory: 16 bytes in, 16 out, four multiply-adds to an 8-byte pair.
-template <typename T, bool INTERLEAVED>
+template <typename T, bool INTERLEAVED, bool ACROSS>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int tile, int heads_per_wg, int stage)
 {
     using V = Row<T>;
     constexpr int E = sizeof(T), EPV = V::kPerVec;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    float2* turns = reinterpret_cast<float2*>(lds);                 // [tile][DP]
-    __shared__ int s_slot[kRotaryTokens];
+    float2* turns = reinterpret_cast<float2*>(lds);                 // [tile][TS]
+    __shared__ int s_slot[kRotaryTokens], s_run[kRotaryTokens], s_runs;
     const int tid = threadIdx.x, D = A.D, n = A.n, half = n / 2;
-    const int DP = (D + EPV - 1) / EPV * EPV;
+    const int DP = (D + EPV - 1) / EPV * EPV, TS = DP + 2;            // (rows of factors start in different banks)
     const bool cached = A.k_cache != nullptr;
     int shift = 0;
     if (cached && tile == kRotaryTokens) {
@@ -107,81 +156,136 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
             turn_of((double)A.positions[t0 + t] * A.sign * A.inv_freq[p], c, s);
             c = (float)(c * A.magnitude);
             s = (float)(s * A.magnitude);
-            turns[t * DP + (INTERLEAVED ? 2 * p : p)] = {c, -s};
-            turns[t * DP + (INTERLEAVED ? 2 * p + 1 : p + half)] = {c, s};
+            turns[t * TS + (INTERLEAVED ? 2 * p : p)] = {c, -s};
+            turns[t * TS + (INTERLEAVED ? 2 * p + 1 : p + half)] = {c, s};
         }
         const int rest = DP - n;
         for (int i = tid; i < tokens * rest; i += 256) {
             const int t = i / rest;
-            turns[t * DP + n + (i - t * rest)] = {1.f, -0.f};
+            turns[t * TS + n + (i - t * rest)] = {1.f, -0.f};
         }
     }
     __syncthreads();
-    const int vecs = DP / EPV, rows = 256 / vecs, row0 = tid / vecs, d0 = (tid - row0 * vecs) * EPV;
-    const int hb = min(h1, turned), hc = hb - h0;                  // heads to turn
+    // One vector of a head row: its loads (no branch around them, so that a batch's are all under way), and what becomes of it.
+    struct Vec {
+        u32x4 own, other, more;
+    };
+    auto load = [&](Vec& v, const char* row, int d0) {
+        v.own = load16_any(row + d0 * E);
+        if constexpr (!INTERLEAVED) {
+            // partners: the vector half a turn further or back; across the middle of the pairs the last of the second half and the first
+            // of the first; dimensions that are only copied fetch themselves
+            const int away = d0 >= n ? d0 : d0 >= half ? d0 - half : d0 + EPV <= half || !ACROSS ? d0 + half : n - EPV;
+            v.other = load16_any(row + away * E);
+            if constexpr (ACROSS) v.more = load16_any(row);
+        }
+    };
+    auto turn = [&](const Vec& v, int t, int d0, float (&f)[EPV]) {
+        float x[EPV], y[EPV];
+        V::unpack(v.own, x);
+        if constexpr (INTERLEAVED) {
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) y[e] = x[e ^ 1];
+        } else {
+            V::unpack(v.other, y);
+            if constexpr (ACROSS) {
+                if (d0 < half && d0 + EPV > half) {
+                    // elements half - d0 from the end of one, the rest from the start of the other
+                    float z[EPV];
+                    V::unpack(v.more, z);
+                    const int k = half - d0;
+#pragma unroll
+                    for (int step = 1; step < EPV; step <<= 1)
+                        if ((EPV - k) & step) {
+#pragma unroll
+                            for (int e = 0; e < EPV; ++e) y[e] = e + step < EPV ? y[e + step] : z[e + step - EPV];
+#pragma unroll
+                            for (int e = 0; e < EPV; ++e) z[e] = e + step < EPV ? z[e + step] : 0.f;
+                        }
+                }
+            }
+        }
+        const float2* w = turns + t * TS + d0;
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) f[e] = fmaf(x[e], w[e].x, (d0 + e < n ? y[e] : 0.f) * w[e].y);
+    };
+    auto k_place = [&](int head, int slot, int d0) {               // of a key's vector in the cache
+        const int page = slot / A.page, off = slot - page * A.page;
+        const int64_t atom = (((int64_t)page * A.kv_heads + head) * (A.page / kAtom) + off / kAtom) * kAtom * D;
+        return reinterpret_cast<u32x4*>((char*)A.k_cache + (atom + (d0 * 2 + off % kAtom) * 8) * 2);
+    };
+    constexpr int BATCH = 4;                                        // vectors whose loads are under way at once
+    const int vecs = DP / EPV;
+    const bool across = cached && stage != 0;                       // keys go to the cache token by token, neighbours in neighbouring lanes
+    const int hb = min(h1, across ? A.q_heads : turned), hc = hb - h0;
+    // (the last vector of a row ends with it; what it shares with the one before is the same twice)
+    auto start_of = [&](int v) { return min(v * EPV, D - EPV); };
+    const int rows = 256 / vecs, row0 = tid / vecs, d0 = start_of(tid - row0 * vecs);
     if (hc > 0 && row0 < rows) {
-        const bool whole = d0 + EPV <= D;
-        // where the vector's partners are: one vector `away` elements further, or (0) here and there, or nowhere (the rest is copied)
-        const bool none = INTERLEAVED || d0 >= n;
-        const int away = none || !whole ? 0 : d0 + EPV <= half ? half : d0 >= half ? -half : 0;
         const int dt = rows / hc, dh = rows - dt * hc;
         int t = row0 / hc, h = row0 - t * hc;
-        for (; t < tokens; t += dt, h += dh) {
-            if (h >= hc) { h -= hc; ++t; if (t >= tokens) break; }
-            const int head = h0 + h, token = t0 + t;
-            const bool isq = head < A.q_heads;
-            const Heads& src = isq ? A.q : A.k;
-            const int sh = isq ? head : head - A.q_heads;
-            const char* row = static_cast<const char*>(src.p) + (token * src.token + sh * src.head) * E;
-            float x[EPV], y[EPV], f[EPV];
-            if (whole) V::unpack(load16_any(row + d0 * E), x);
-            else {
+        while (t < tokens) {
+            Vec v[BATCH];
+            int at[BATCH], tok[BATCH];
 #pragma unroll
-                for (int e = 0; e < EPV; ++e) x[e] = d0 + e < D ? V::load(row + (d0 + e) * E) : 0.f;
+            for (int u = 0; u < BATCH; ++u) {
+                tok[u] = min(t, tokens - 1);
+                at[u] = t < tokens ? h0 + h : -1;
+                const int head = h0 + h, token = t0 + tok[u];
+                const bool isq = head < A.q_heads;
+                const char* p = static_cast<const char*>(isq ? A.q.p : A.k.p);
+                const int64_t ts = isq ? A.q.token : A.k.token, hs = isq ? A.q.head : A.k.head;
+                load(v[u], p + (token * ts + (isq ? head : head - A.q_heads) * hs) * E, d0);
+                t += dt;
+                h += dh;
+                if (h >= hc) { h -= hc; ++t; }
             }
-            if constexpr (INTERLEAVED) {
 #pragma unroll
-                for (int e = 0; e < EPV; ++e) y[e] = d0 + e < n ? x[e ^ 1] : 0.f;
-            } else {
-                if (away != 0) {
-                    V::unpack(load16_any(row + (d0 + away) * E), y);
-#pragma unroll
-                    for (int e = 0; e < EPV; ++e) y[e] = d0 + e < n ? y[e] : 0.f;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < EPV; ++e) {
-                        const int d = d0 + e;
-                        y[e] = none || d >= n ? 0.f : V::load(row + (d < half ? d + half : d - half) * E);
-                    }
-                }
-            }
-            const float2* w = turns + t * DP + d0;
-#pragma unroll
-            for (int e = 0; e < EPV; ++e) f[e] = fmaf(x[e], w[e].x, y[e] * w[e].y);
-            if (isq || !cached) {
-                const Heads& dst = isq ? A.q_out : A.k_out;
-                char* o = (char*)dst.p + (token * dst.token + sh * dst.head + d0) * E;
+            for (int u = 0; u < BATCH; ++u) {
+                float f[EPV];
+                turn(v[u], tok[u], d0, f);
+                const bool isq = at[u] < A.q_heads;
+                const int token = t0 + tok[u], head = isq ? at[u] : at[u] - A.q_heads;
                 const u32x4 r = V::pack(f);
-                if (whole) __builtin_memcpy(o, &r, 16);
-                else {
-#pragma unroll
-                    for (int e = 0; e < EPV; ++e)
-                        if (d0 + e < D) V::store(o + e * E, f[e]);
-                }
-            } else if (E == 2) {
-                const int slot = s_slot[t];
-                if (slot >= 0) {
-                    const int page = slot / A.page, off = slot - page * A.page;
-                    const int64_t atom = (((int64_t)page * A.kv_heads + sh) * (A.page / kAtom) + off / kAtom) * kAtom * D;
-                    *reinterpret_cast<u32x4*>((char*)A.k_cache + (atom + (d0 * 2 + off % kAtom) * 8) * 2) = V::pack(f);
+                if (at[u] < 0) continue;
+                if (isq || !cached) {
+                    char* p = (char*)(isq ? A.q_out.p : A.k_out.p);
+                    const int64_t ts = isq ? A.q_out.token : A.k_out.token, hs = isq ? A.q_out.head : A.k_out.head;
+                    __builtin_memcpy(p + (token * ts + head * hs + d0) * E, &r, 16);
+                } else if (E == 2) {
+                    const int slot = s_slot[tok[u]];
+                    if (slot >= 0) *k_place(head, slot, d0) = r;
                 }
             }
         }
     }
     if (!cached || E != 2) return;
+    const int k0 = max(h0, A.q_heads), k1 = min(h1, turned), v0 = max(h0, turned);
+    if (across && k0 < k1) {
+        // (sixteen tokens' 16 bytes are 256 consecutive bytes of an atom)
+        const int t = tid & 15, count = (k1 - k0) * vecs, slot = t < tokens ? s_slot[t] : -1;
+        if (slot >= 0)
+            for (int i = tid >> 4; i < count; i += 16 * BATCH) {
+                Vec v[BATCH];
+                int head[BATCH], from[BATCH];
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    const int j = min(i + 16 * u, count - 1);
+                    head[u] = k0 - A.q_heads + j / vecs;
+                    from[u] = j % vecs * EPV;
+                    load(v[u], static_cast<const char*>(A.k.p) + ((t0 + t) * A.k.token + head[u] * A.k.head) * E, from[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    float f[EPV];
+                    turn(v[u], t, from[u], f);
+                    if (i + 16 * u < count) *k_place(head[u], slot, from[u]) = V::pack(f);
+                }
+            }
+    }
     // the values
-    const int v0 = max(h0, turned);
-    if (stage == 0) {
+    if (v0 >= h1) return;
+    if (!across) {
         // (few tokens: element by element)
         for (int h = v0; h < h1; ++h)
             for (int i = tid; i < tokens * D; i += 256) {
@@ -194,41 +298,58 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
             }
         return;
     }
-    if (v0 >= h1) return;
-    // runs of consecutive slots within eight: a thread takes a dimension of a run
+    // Runs of consecutive slots within eight: a thread takes a dimension of a run.
+    if (tid < 64) {
+        const int slot = tid < tokens ? s_slot[tid] : -1, before = tid > 0 ? s_slot[max(tid, 1) - 1] : -2;
+        const bool starts = slot >= 0 && (tid == 0 || before + 1 != slot || slot % 8 == 0 || before < 0);
+        const unsigned long long all_starts = __ballot(starts), held = __ballot(slot >= 0);
+        if (starts) {
+            const unsigned long long stops = (all_starts | ~held) >> tid >> 1;        // (bit 16 at the latest)
+            s_run[__popcll(all_starts & ((1ull << tid) - 1))] = tid | (__ffsll((long long)stops) << 8);
+        }
+        if (tid == 0) s_runs = __popcll(all_starts);
+    }
     const int RS = D + 2;                                           // halves of a staged row (rows of a column in different banks)
+    const int at_once = stage / (kRotaryTokens * RS * 2), per = D / 8;
     uint16_t* staged = reinterpret_cast<uint16_t*>(lds);
-    const int ds = 256 / D > 0 ? 256 / D : 1;
-    for (int h = v0; h < h1; ++h) {
+    const int lanes = D <= 256 ? 256 / D : 1;                       // runs taken side by side
+    for (int hv = v0; hv < h1; hv += at_once) {
+        const int nh = min(at_once, h1 - hv);
         __syncthreads();
-        for (int i = tid; i < tokens * (D / 8); i += 256) {
-            const int t = i / (D / 8), d = (i - t * (D / 8)) * 8;
-            const u32x4 r = load16_any(static_cast<const char*>(A.v.p) + ((t0 + t) * A.v.token + (h - turned) * A.v.head + d) * 2);
-            uint32_t* to = reinterpret_cast<uint32_t*>(staged + t * RS + d);
+        for (int i = tid; i < nh * tokens * per; i += 256 * BATCH) {
+            u32x4 r[BATCH];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) to[e] = r[e];
+            for (int u = 0; u < BATCH; ++u) {
+                const int j = min(i + 256 * u, nh * tokens * per - 1), row = j / per, t = row / nh, h = row - t * nh;
+                r[u] = load16_any(static_cast<const char*>(A.v.p) + ((t0 + t) * A.v.token + (hv + h - turned) * A.v.head + (j - row * per) * 8) * 2);
+            }
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const int j = i + 256 * u, row = j / per, t = row / nh, h = row - t * nh;
+                if (j >= nh * tokens * per) break;
+                uint32_t* to = reinterpret_cast<uint32_t*>(staged + (h * kRotaryTokens + t) * RS + (j - row * per) * 8);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[e] = r[u][e];
+            }
         }
         __syncthreads();
-        for (int run = 0, t = 0; t < tokens; ++run) {
-            const int slot = s_slot[t];
-            int len = 1;
-            while (t + len < tokens && slot >= 0 && (slot + len) % 8 != 0 && s_slot[t + len] == slot + len) ++len;
-            if (slot >= 0 && (ds == 1 || run % ds == tid / D)) {
-                const int page = slot / A.page, off = slot - page * A.page, at = off % kAtom;
-                const int64_t atom = (((int64_t)page * A.kv_heads + h - turned) * (A.page / kAtom) + off / kAtom) * kAtom * D;
-                for (int d = ds == 1 ? tid : tid % D; d < D; d += ds == 1 ? 256 : D) {
-                    uint16_t* to = reinterpret_cast<uint16_t*>(A.v_cache) + atom + (at / 8 * D + d) * 8 + at % 8;
-                    const uint16_t* from = staged + t * RS + d;
-                    if (len == 8) {
-                        u32x4 r;
+        const int jobs = nh * s_runs;
+        for (int j = lanes > 1 ? tid / D : 0; j < jobs; j += lanes) {
+            if (lanes > 1 && tid >= lanes * D) break;
+            const int h = j / s_runs, run = s_run[j - h * s_runs], t = run & 0xff, len = run >> 8, slot = s_slot[t];
+            const int page = slot / A.page, off = slot - page * A.page, at = off % kAtom;
+            const int64_t atom = (((int64_t)page * A.kv_heads + hv + h - turned) * (A.page / kAtom) + off / kAtom) * kAtom * D;
+            for (int d = lanes > 1 ? tid % D : tid; d < D; d += lanes > 1 ? D : 256) {
+                uint16_t* to = reinterpret_cast<uint16_t*>(A.v_cache) + atom + (at / 8 * D + d) * 8 + at % 8;
+                const uint16_t* from = staged + (h * kRotaryTokens + t) * RS + d;
+                if (len == 8) {
+                    u32x4 r;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) r[e] = from[2 * e * RS] | (uint32_t)from[(2 * e + 1) * RS] << 16;
-                        *reinterpret_cast<u32x4*>(to) = r;
-                    } else
-                        for (int e = 0; e < len; ++e) to[e] = from[e * RS];
-                }
+                    for (int e = 0; e < 4; ++e) r[e] = from[2 * e * RS] | (uint32_t)from[(2 * e + 1) * RS] << 16;
+                    *reinterpret_cast<u32x4*>(to) = r;
+                } else
+                    for (int e = 0; e < len; ++e) to[e] = from[e * RS];
             }
-            t += len;
         }
     }
 }
@@ -240,6 +361,17 @@ hipError_t launch_rotary(int dtype, bool interleaved, const RotaryArgs& args, hi
     if (args.T <= 0) return hipSuccess;
     const bool cached = args.k_cache != nullptr;
     const int heads = args.q_heads + args.kv_heads + (cached ? args.kv_heads : 0), cus = compute_units();
+    if (args.D < 2 * (dtype == 0 ? 4 : 8) || args.n < (dtype == 0 ? 4 : 8) || (interleaved && args.D % 2 != 0)) {
+        const dim3 g((unsigned)args.T), b(256);
+        if (dtype == 0) {
+            if (interleaved) hipLaunchKernelGGL((rotary_short_kernel<float, true>), g, b, 0, stream, args);
+            else hipLaunchKernelGGL((rotary_short_kernel<float, false>), g, b, 0, stream, args);
+        } else {
+            if (interleaved) hipLaunchKernelGGL((rotary_short_kernel<bf16_t, true>), g, b, 0, stream, args);
+            else hipLaunchKernelGGL((rotary_short_kernel<bf16_t, false>), g, b, 0, stream, args);
+        }
+        return hipGetLastError();
+    }
     // Tokens of a workgroup: 16 where they still make a workgroup for every compute unit (the cache's atoms whole, the factors of a
     // token computed for many heads), 1 where they do not.  Heads: as many ranges as make eight workgroups a unit.
     int tile = args.T >= kRotaryTokens * (cus / 4) ? kRotaryTokens : 1;
@@ -250,16 +382,23 @@ hipError_t launch_rotary(int dtype, bool interleaved, const RotaryArgs& args, hi
     if (ranges > (heads + 1) / 2) ranges = (heads + 1) / 2;
     if (ranges < 1) ranges = 1;
     const int each = (int)((heads + ranges - 1) / ranges);
-    const int stage = tile == kRotaryTokens ? tile * (args.D + 2) * 2 : 0;
-    const int bytes = tile * DP * 8 > stage ? tile * DP * 8 : stage;
+    // (values are staged where the factors were: as many heads at a time as fit, at least one)
+    const int factors = tile * (DP + 2) * 8, one = kRotaryTokens * (args.D + 2) * 2;
+    const int stage = cached && tile == kRotaryTokens ? (factors > one ? factors / one * one : one) : 0;
+    const int bytes = factors > stage ? factors : stage;
     const dim3 grid((unsigned)tiles, (unsigned)((heads + each - 1) / each)), block(256);
+#define CIAR_ROTARY(T, I, X) hipLaunchKernelGGL((rotary_kernel<T, I, X>), grid, block, bytes, stream, args, tile, each, stage)
+    const bool across = args.n / 2 % per != 0;
     if (dtype == 0) {
-        if (interleaved) hipLaunchKernelGGL((rotary_kernel<float, true>), grid, block, bytes, stream, args, tile, each, stage);
-        else hipLaunchKernelGGL((rotary_kernel<float, false>), grid, block, bytes, stream, args, tile, each, stage);
+        if (interleaved) CIAR_ROTARY(float, true, false);
+        else if (across) CIAR_ROTARY(float, false, true);
+        else CIAR_ROTARY(float, false, false);
     } else {
-        if (interleaved) hipLaunchKernelGGL((rotary_kernel<bf16_t, true>), grid, block, bytes, stream, args, tile, each, stage);
-        else hipLaunchKernelGGL((rotary_kernel<bf16_t, false>), grid, block, bytes, stream, args, tile, each, stage);
+        if (interleaved) CIAR_ROTARY(bf16_t, true, false);
+        else if (across) CIAR_ROTARY(bf16_t, false, true);
+        else CIAR_ROTARY(bf16_t, false, false);
     }
+#undef CIAR_ROTARY
     return hipGetLastError();
 }
 
