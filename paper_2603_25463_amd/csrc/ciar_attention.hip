@@ -934,18 +934,21 @@ Shape shape_of(const AttentionArgs& a)
     return s;
 }
 
-// Asks once per device for the dynamic LDS that a kernel needs.
-hipError_t allow_lds(const void* kernel, int bytes)
-{
-    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-
 template <int D, int QT>
 hipError_t launch_many(const AttentionArgs& a, const Shape& s, unsigned grid, int64_t work, float* po, float2* ps, hipStream_t stream)
 {
     constexpr int bytes = (D <= 128 ? 5 : 4) * 4 * kAtom * D * 2;
-    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&many_rows_kernel<D, QT>), bytes);
-    if (e != hipSuccess) return e;
+    {
+        // more than the default limit for dynamic LDS: raised for this kernel once per device
+        static std::atomic<bool> raised[64];
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
+        if (!raised[dev].load(std::memory_order_acquire)) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&many_rows_kernel<D, QT>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+            if (e != hipSuccess) return e;
+            raised[dev].store(true, std::memory_order_release);
+        }
+    }
     hipLaunchKernelGGL((many_rows_kernel<D, QT>), dim3(grid), dim3(256), bytes, stream, a, pages_of(a.page), s.blocks, s.splits, work, po, ps);
     return hipGetLastError();
 }

@@ -373,12 +373,13 @@ hipError_t launch_rotary(int dtype, bool interleaved, const RotaryArgs& args, hi
         return hipGetLastError();
     }
     // Tokens of a workgroup: 16 where they still make a workgroup for every compute unit (the cache's atoms whole, the factors of a
-    // token computed for many heads), 1 where they do not.  Heads: as many ranges as make eight workgroups a unit.
+    // token computed for many heads), 1 where they do not.  Heads: as many ranges as make four workgroups a unit (8192 tokens, 48 heads: 2 a unit 62.5 us, 4 54.5,
+    // 8 57.2, 16 58.5).
     int tile = args.T >= kRotaryTokens * (cus / 4) ? kRotaryTokens : 1;
     if (args.D > 256 && tile > 4) tile = 4;                         // (factors of 8 bytes a dimension: 32 KiB of LDS)
     const int per = dtype == 0 ? 4 : 8, DP = (args.D + per - 1) / per * per;
     const int64_t tiles = ((int64_t)args.T + tile - 1) / tile + (cached && tile == kRotaryTokens ? 1 : 0);
-    int64_t ranges = (8 * (int64_t)cus + tiles - 1) / tiles;
+    int64_t ranges = (4 * (int64_t)cus + tiles - 1) / tiles;
     if (ranges > (heads + 1) / 2) ranges = (heads + 1) / 2;
     if (ranges < 1) ranges = 1;
     const int each = (int)((heads + ranges - 1) / ranges);

@@ -1,0 +1,601 @@
+// The verification step's operators as Python functions of torch tensors: checks of types, shapes and devices, output tensors, the C
+// ABI's call (include/ciar.h).  Native because these calls are short: eight requests' plan is 4 us of kernel, and with the checks of
+// its 17 tensors in Python the call took 15.5.
+#include <Python.h>
+
+#include <ATen/ATen.h>
+#include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <cmath>
+#include <string>
+
+#include "../../include/ciar.h"
+
+namespace {
+
+// A Python exception to be raised: its class and text (none: already set).
+struct Raise {
+    PyObject* type;
+    std::string text;
+};
+[[noreturn]] void value_error(const std::string& text) { throw Raise{PyExc_ValueError, text}; }
+[[noreturn]] void type_error(const std::string& text) { throw Raise{PyExc_TypeError, text}; }
+[[noreturn]] void pending() { throw Raise{nullptr, ""}; }
+
+std::string shape_of(const at::Tensor& t)
+{
+    std::string s = "(";
+    for (int64_t i = 0; i < t.dim(); ++i) s += (i ? ", " : "") + std::to_string(t.size(i));
+    return s + ")";
+}
+const char* type_name(at::ScalarType t)
+{
+    switch (t) {
+        case at::kInt: return "torch.int32";
+        case at::kLong: return "torch.int64";
+        case at::kByte: return "torch.uint8";
+        case at::kFloat: return "torch.float32";
+        case at::kDouble: return "torch.float64";
+        case at::kBFloat16: return "torch.bfloat16";
+        default: return c10::toString(t);
+    }
+}
+
+// ---- arguments ----------------------------------------------------------------------------------------------------
+
+// The arguments of a call, in the order of `names` (borrowed; null where not given).
+template <int N>
+struct Args {
+    PyObject* v[N] = {};
+
+    Args(const char* function, PyObject* const (&names)[N], int positional, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
+    {
+        if (nargs > positional)
+            type_error(std::string(function) + "() takes " + std::to_string(positional) + " positional arguments but " + std::to_string(nargs) + " were given");
+        for (Py_ssize_t i = 0; i < nargs; ++i) v[i] = args[i];
+        const Py_ssize_t nkw = kwnames ? PyTuple_GET_SIZE(kwnames) : 0;
+        for (Py_ssize_t k = 0; k < nkw; ++k) {
+            PyObject* name = PyTuple_GET_ITEM(kwnames, k);
+            int i = 0;
+            while (i < N && names[i] != name) ++i;                  // (both are interned, nearly always)
+            for (int j = 0; i == N && j < N; ++j)
+                if (PyUnicode_Compare(names[j], name) == 0) { i = j; break; }
+            if (i == N) type_error(std::string(function) + "() got an unexpected keyword argument '" + PyUnicode_AsUTF8(name) + "'");
+            if (v[i]) type_error(std::string(function) + "() got multiple values for argument '" + PyUnicode_AsUTF8(name) + "'");
+            v[i] = args[nargs + k];
+        }
+    }
+    bool given(int i) const { return v[i] && v[i] != Py_None; }
+};
+
+template <int N>
+void require(const char* function, PyObject* const (&names)[N], const Args<N>& a, std::initializer_list<int> needed)
+{
+    for (int i : needed)
+        if (!a.v[i]) type_error(std::string(function) + "() missing required argument: '" + PyUnicode_AsUTF8(names[i]) + "'");
+}
+
+const at::Tensor& tensor(PyObject* o, const char* name)
+{
+    if (!THPVariable_Check(o)) type_error(std::string(name) + " must be a tensor");
+    return THPVariable_Unpack(o);
+}
+int64_t integer(PyObject* o, const char* name)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        PyObject* i = PyNumber_Index(o);                            // (numpy integers and the like)
+        if (!i) { PyErr_Clear(); type_error(std::string(name) + " must be an integer"); }
+        const long long w = PyLong_AsLongLong(i);
+        Py_DECREF(i);
+        if (w == -1 && PyErr_Occurred()) { PyErr_Clear(); value_error(std::string(name) + " is out of range"); }
+        return w;
+    }
+    return v;
+}
+int32_t integer32(PyObject* o, const char* name)
+{
+    const int64_t v = integer(o, name);
+    if (v < INT32_MIN || v > INT32_MAX) value_error(std::string(name) + " is out of range");
+    return (int32_t)v;
+}
+double number(PyObject* o, const char* name)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); type_error(std::string(name) + " must be a number"); }
+    return v;
+}
+void on_gpu(const at::Tensor& t)
+{
+    if (!t.is_cuda()) value_error("all tensors must live on the GPU");
+}
+// The pointer of a contiguous list of n values (n < 0: of any length).
+void* list(const at::Tensor& t, const char* name, at::ScalarType type, int64_t n)
+{
+    if (t.scalar_type() != type || t.dim() != 1 || (n >= 0 && t.size(0) != n) || !t.is_contiguous())
+        value_error(std::string(name) + " must be a contiguous " + type_name(type) + " tensor of " + (n < 0 ? std::string("any number of") : std::to_string(n)) +
+                    " entries, got " + type_name(t.scalar_type()) + " " + shape_of(t));
+    on_gpu(t);
+    return t.data_ptr();
+}
+void* list(PyObject* o, const char* name, at::ScalarType type, int64_t n) { return list(tensor(o, name), name, type, n); }
+// An int32 matrix with unit stride along its rows.
+void* matrix(const at::Tensor& t, const char* name)
+{
+    if (t.scalar_type() != at::kInt || t.dim() != 2 || (t.stride(1) != 1 && t.size(1) > 1))
+        value_error(std::string(name) + " must be a 2-D int32 tensor with unit stride along its rows");
+    on_gpu(t);
+    return t.data_ptr();
+}
+// Elements between rows (a single row's stride means nothing: at least its length).
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1)); }
+// A [T, heads, D] tensor whose heads' dimensions are consecutive.
+void* head_rows(const at::Tensor& t, const char* name, at::ScalarType type, int64_t T, int64_t heads, int64_t D)
+{
+    if (t.scalar_type() != type) type_error(std::string(name) + " must be " + type_name(type) + ", got " + type_name(t.scalar_type()));
+    if (t.dim() != 3 || t.size(0) != T || (heads >= 0 && t.size(1) != heads) || t.size(2) != D || (t.stride(2) != 1 && D > 1))
+        value_error(std::string(name) + " must be [" + std::to_string(T) + ", " + (heads < 0 ? std::string("heads") : std::to_string(heads)) + ", " +
+                    std::to_string(D) + "] with unit stride along the last dimension, got " + shape_of(t));
+    on_gpu(t);
+    return t.data_ptr();
+}
+
+struct Cache {
+    void *k, *v;
+    int64_t pages, heads, page, dim;
+};
+Cache cache(PyObject* ko, PyObject* vo)
+{
+    const at::Tensor &k = tensor(ko, "k_cache"), &v = tensor(vo, "v_cache");
+    if (k.scalar_type() != at::kBFloat16 || v.scalar_type() != at::kBFloat16) type_error("k_cache and v_cache must be bfloat16");
+    const auto s = k.sizes(), z = v.sizes();
+    if (s.size() != 6 || z.size() != 6 || s[4] != 16 || s[5] != 8 || z[0] != s[0] || z[1] != s[1] || z[2] != s[2] || z[3] != 2 || z[4] != 8 * s[3] || z[5] != 8)
+        value_error("k_cache must be [pages, kv_heads, page_size / 16, head_dim / 8, 16, 8] and v_cache "
+                    "[pages, kv_heads, page_size / 16, 2, head_dim, 8], got " + shape_of(k) + " and " + shape_of(v));
+    if (!k.is_contiguous() || !v.is_contiguous()) value_error("k_cache and v_cache must be contiguous");
+    on_gpu(k);
+    on_gpu(v);
+    if (s[1] > INT32_MAX || s[2] > INT32_MAX / 16 || s[3] > INT32_MAX / 8) value_error("k_cache is too large");
+    return {k.data_ptr(), v.data_ptr(), s[0], s[1], s[2] * 16, s[3] * 8};
+}
+
+// ---- outputs, stream, errors ---------------------------------------------------------------------------------------
+
+// The dictionary that a call returns: a copy of what `out` brings, completed by what it does not.
+struct Outputs {
+    PyObject* dict;
+    explicit Outputs(PyObject* out)
+    {
+        if (out && out != Py_None && !PyDict_Check(out)) type_error("out must be a dict");
+        dict = out && out != Py_None ? PyDict_Copy(out) : PyDict_New();
+        if (!dict) pending();
+    }
+    ~Outputs() { Py_XDECREF(dict); }
+    Outputs(const Outputs&) = delete;
+    PyObject* get(PyObject* name) const
+    {
+        PyObject* o = PyDict_GetItemWithError(dict, name);
+        return o == Py_None ? nullptr : o;
+    }
+    template <class Make>
+    const at::Tensor& get(PyObject* name, const char* what, Make make)
+    {
+        PyObject* o = get(name);
+        if (!o) {
+            o = THPVariable_Wrap(make());
+            if (!o) pending();
+            const int rc = PyDict_SetItem(dict, name, o);
+            Py_DECREF(o);                                           // (the dictionary holds it)
+            if (rc != 0) pending();
+        }
+        return tensor(o, what);
+    }
+    PyObject* release()
+    {
+        PyObject* d = dict;
+        dict = nullptr;
+        return d;
+    }
+};
+
+at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& like)
+{
+    return at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
+}
+
+PyObject *s_window, *s_cuda_stream, *s_half, *s_interleaved;
+
+void* stream_of(PyObject* o)
+{
+    if (!o || o == Py_None) return c10::hip::getCurrentHIPStream().stream();
+    PyObject* handle = PyObject_GetAttr(o, s_cuda_stream);
+    if (!handle) pending();
+    void* s = PyLong_AsVoidPtr(handle);
+    Py_DECREF(handle);
+    if (!s && PyErr_Occurred()) pending();
+    return s;
+}
+
+// The caller's workspace, or a fresh one of `need` bytes (held by `keep`; the allocator reuses it in the order of the stream).
+void* workspace_of(PyObject* o, size_t need, const at::Tensor& like, at::Tensor& keep, size_t& bytes)
+{
+    if (o && o != Py_None) {
+        const at::Tensor& t = tensor(o, "workspace");
+        if (!t.is_cuda() || !t.is_contiguous()) value_error("workspace must be a contiguous tensor on the GPU");
+        bytes = (size_t)t.nbytes();
+        return t.data_ptr();
+    }
+    bytes = need;
+    if (!need) return nullptr;
+    keep = empty({(int64_t)need}, at::kByte, like);
+    return keep.data_ptr();
+}
+
+void check(int rc)
+{
+    if (rc == CIAR_OK) return;
+    PyObject* module = PyImport_ImportModule("paper_2603_25463_amd.binding");
+    PyObject* cls = module ? PyObject_GetAttrString(module, "CiarError") : nullptr;
+    PyObject* e = cls ? PyObject_CallFunction(cls, "is", rc, ciar_last_error()) : nullptr;
+    if (e) PyErr_SetObject(cls, e);
+    Py_XDECREF(e);
+    Py_XDECREF(cls);
+    Py_XDECREF(module);
+    pending();
+}
+
+template <class F>
+PyObject* guarded(F f)
+{
+    try {
+        return f();
+    } catch (const Raise& r) {
+        if (r.type) PyErr_SetString(r.type, r.text.c_str());
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown C++ exception");
+    }
+    return nullptr;
+}
+
+// ---- the operators -----------------------------------------------------------------------------------------------
+
+enum { P_LENGTHS, P_NEW, P_HELD, P_RING, P_STATE, P_TABLE, P_TOKENS, P_PAGE, P_KEPT, P_STREAM, P_OUT, P_COUNT };
+PyObject* plan_names[P_COUNT];
+enum { PO_LENGTHS, PO_KV, PO_CU, PO_HELD, PO_GRANTED, PO_STATE, PO_SLOTS, PO_POSITIONS, PO_REQUESTS, PO_COUNT };
+PyObject* plan_outputs[PO_COUNT];
+
+PyObject* cache_plan(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
+{
+    return guarded([&]() -> PyObject* {
+        Args<P_COUNT> a("cache_plan", plan_names, P_PAGE, args, nargs, kwnames);
+        require("cache_plan", plan_names, a, {P_LENGTHS, P_NEW, P_HELD, P_RING, P_STATE, P_TABLE, P_TOKENS, P_PAGE});
+        const at::Tensor &lengths = tensor(a.v[P_LENGTHS], "lengths"), &table = tensor(a.v[P_TABLE], "table"), &ring = tensor(a.v[P_RING], "ring");
+        if (lengths.dim() != 1) value_error("lengths must be a contiguous torch.int32 tensor, got " + shape_of(lengths));
+        const int64_t R = lengths.size(0), T = integer(a.v[P_TOKENS], "tokens");
+        if (T < 0) value_error("tokens is negative");
+        const auto* lp = (const int32_t*)list(lengths, "lengths", at::kInt, R);
+        const auto* kp = a.given(P_KEPT) ? (const int32_t*)list(a.v[P_KEPT], "kept", at::kInt, R) : nullptr;
+        const auto* np = (const int32_t*)list(a.v[P_NEW], "new", at::kInt, R);
+        const auto* hp = (const int32_t*)list(a.v[P_HELD], "held", at::kInt, R);
+        auto* rp = (int32_t*)list(ring, "ring", at::kInt, -1);
+        const auto* sp = (const int64_t*)list(a.v[P_STATE], "ring_state", at::kLong, 2);
+        auto* tp = (int32_t*)matrix(table, "table");
+        if (table.size(0) != R) value_error("table must have " + std::to_string(R) + " rows, got " + std::to_string(table.size(0)));
+        if (table.size(1) > INT32_MAX) value_error("table is too wide");
+        static const struct { const char* name; at::ScalarType type; } what[PO_COUNT] = {
+            {"out['lengths']", at::kInt}, {"out['kv_len']", at::kInt}, {"out['cu_new']", at::kInt}, {"out['held']", at::kInt}, {"out['granted']", at::kByte},
+            {"out['ring_state']", at::kLong}, {"out['slots']", at::kInt}, {"out['positions']", at::kInt}, {"out['requests']", at::kInt}};
+        Outputs o(a.v[P_OUT]);
+        void* p[PO_COUNT];
+        for (int i = 0; i < PO_COUNT; ++i) {
+            const int64_t n = i == PO_CU ? R + 1 : i == PO_STATE ? 2 : i >= PO_SLOTS ? T : R;
+            p[i] = list(o.get(plan_outputs[i], what[i].name, [&] { return empty({n}, what[i].type, lengths); }), what[i].name, what[i].type, n);
+        }
+        const int32_t page = integer32(a.v[P_PAGE], "page_size");
+        void* stream = stream_of(a.v[P_STREAM]);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = ciar_cache_plan(lp, kp, np, hp, R, rp, ring.numel(), sp, tp, (int32_t)table.size(1), row_stride(table), page, T, (int32_t*)p[PO_LENGTHS],
+                             (int32_t*)p[PO_KV], (int32_t*)p[PO_CU], (int32_t*)p[PO_HELD], (uint8_t*)p[PO_GRANTED], (int64_t*)p[PO_STATE],
+                             (int32_t*)p[PO_SLOTS], (int32_t*)p[PO_POSITIONS], (int32_t*)p[PO_REQUESTS], stream);
+        Py_END_ALLOW_THREADS
+        check(rc);
+        return o.release();
+    });
+}
+
+enum { R_Q, R_K, R_POSITIONS, R_FREQ, R_LAYOUT, R_INVERSE, R_MAGNITUDE, R_V, R_KC, R_VC, R_SLOTS, R_STREAM, R_OUT, R_COUNT };
+PyObject* rotary_names[R_COUNT];
+
+PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
+{
+    return guarded([&]() -> PyObject* {
+        Args<R_COUNT> a("rotary", rotary_names, R_LAYOUT, args, nargs, kwnames);
+        require("rotary", rotary_names, a, {R_Q, R_K, R_POSITIONS, R_FREQ});
+        const at::Tensor &q = tensor(a.v[R_Q], "q"), &k = tensor(a.v[R_K], "k"), &freq = tensor(a.v[R_FREQ], "inv_freq");
+        bool interleaved = false;
+        if (a.v[R_LAYOUT]) {
+            if (!PyUnicode_Check(a.v[R_LAYOUT])) type_error("layout must be a string");
+            interleaved = PyUnicode_Compare(a.v[R_LAYOUT], s_interleaved) == 0;
+            if (!interleaved && PyUnicode_Compare(a.v[R_LAYOUT], s_half) != 0)
+                value_error(std::string("layout must be 'half' or 'interleaved', got '") + PyUnicode_AsUTF8(a.v[R_LAYOUT]) + "'");
+        }
+        const int inverse = a.v[R_INVERSE] ? PyObject_IsTrue(a.v[R_INVERSE]) : 0;
+        if (inverse < 0) pending();
+        if (q.dim() != 3 || k.dim() != 3) value_error("q and k must be [T, heads, D]");
+        const at::ScalarType type = q.scalar_type();
+        if (type != at::kBFloat16 && type != at::kFloat) type_error(std::string("q must be float32 or bfloat16, got ") + type_name(type));
+        const int64_t T = q.size(0), Hq = q.size(1), D = q.size(2), Hk = k.size(1);
+        if (Hq > INT32_MAX || Hk > INT32_MAX || D > INT32_MAX) value_error("q or k is too large");
+        ciar_rotary_params p = {};
+        p.struct_size = sizeof p;
+        p.dtype = type == at::kFloat ? CIAR_F32 : CIAR_BF16;
+        p.q_heads = (int32_t)Hq;
+        p.kv_heads = (int32_t)Hk;
+        p.head_dim = (int32_t)D;
+        p.interleaved = interleaved;
+        p.inverse = inverse;
+        p.magnitude = a.v[R_MAGNITUDE] ? number(a.v[R_MAGNITUDE], "magnitude") : 1.0;
+        const void *qp = head_rows(q, "q", type, T, Hq, D), *kp = head_rows(k, "k", type, T, Hk, D), *vp = nullptr;
+        const auto* pp = (const int32_t*)list(a.v[R_POSITIONS], "positions", at::kInt, T);
+        const auto* fp = (const double*)list(freq, "inv_freq", at::kDouble, -1);
+        if (freq.numel() > INT32_MAX / 2) value_error("inv_freq is too long");
+        p.rotary_dim = (int32_t)(2 * freq.numel());
+        Outputs o(a.v[R_OUT]);
+        const at::Tensor& qo = o.get(rotary_names[R_Q], "out['q']", [&] { return empty({T, Hq, D}, type, q); });
+        void *qop = head_rows(qo, "out['q']", type, T, Hq, D), *kop = nullptr;
+        Cache c = {};
+        const int32_t* slots = nullptr;
+        if (a.given(R_KC) || a.given(R_VC) || a.given(R_SLOTS)) {
+            if (!(a.given(R_KC) && a.given(R_VC) && a.given(R_SLOTS) && a.given(R_V))) value_error("v, k_cache, v_cache and slots go together");
+            if (o.get(rotary_names[R_K])) value_error("out['k'] is not written where a cache is given");
+            c = cache(a.v[R_KC], a.v[R_VC]);
+            if (c.heads != Hk || c.dim != D)
+                value_error("the cache has " + std::to_string(c.heads) + " heads of " + std::to_string(c.dim) + ", k has " + std::to_string(Hk) + " of " + std::to_string(D));
+            const at::Tensor& v = tensor(a.v[R_V], "v");
+            vp = head_rows(v, "v", type, T, Hk, D);
+            slots = (const int32_t*)list(a.v[R_SLOTS], "slots", at::kInt, T);
+            p.page_size = (int32_t)c.page;
+            p.cache_pages = c.pages;
+            p.v_stride = v.stride(0);
+            p.v_head_stride = v.stride(1);
+        } else {
+            if (a.given(R_V)) value_error("v is given without a cache");
+            const at::Tensor& ko = o.get(rotary_names[R_K], "out['k']", [&] { return empty({T, Hk, D}, type, q); });
+            kop = head_rows(ko, "out['k']", type, T, Hk, D);
+            p.k_out_stride = ko.stride(0);
+            p.k_out_head_stride = ko.stride(1);
+        }
+        p.q_stride = q.stride(0);
+        p.q_head_stride = q.stride(1);
+        p.k_stride = k.stride(0);
+        p.k_head_stride = k.stride(1);
+        p.q_out_stride = qo.stride(0);
+        p.q_out_head_stride = qo.stride(1);
+        void* stream = stream_of(a.v[R_STREAM]);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = ciar_rotary(qp, kp, vp, pp, fp, T, &p, qop, kop, c.k, c.v, slots, stream);
+        Py_END_ALLOW_THREADS
+        check(rc);
+        return o.release();
+    });
+}
+
+enum { A_Q, A_KC, A_VC, A_TABLE, A_CU, A_LEN, A_MAXNEW, A_MAXLEN, A_SCALE, A_STREAM, A_OUT, A_WORKSPACE, A_COUNT };
+PyObject* attention_names[A_COUNT];
+PyObject *s_out, *s_lse;
+
+// The sizes of an attention call.
+ciar_attention_params attention_params(const at::Tensor& q, const Cache& c, const at::Tensor& table, PyObject* max_new, PyObject* max_len)
+{
+    if (q.dim() != 3) value_error("q must be [T, heads, D]");
+    if (q.size(1) > INT32_MAX || table.size(1) > INT32_MAX) value_error("q or table is too large");
+    ciar_attention_params p = {};
+    p.struct_size = sizeof p;
+    p.q_heads = (int32_t)q.size(1);
+    p.kv_heads = (int32_t)c.heads;
+    p.head_dim = (int32_t)c.dim;
+    p.page_size = (int32_t)c.page;
+    p.table_width = (int32_t)table.size(1);
+    p.max_new = integer32(max_new, "max_new");
+    p.max_len = integer32(max_len, "max_len");
+    p.table_stride = row_stride(table);
+    p.cache_pages = c.pages;
+    p.scale = (float)(1.0 / std::sqrt((double)c.dim));
+    return p;
+}
+
+PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
+{
+    return guarded([&]() -> PyObject* {
+        Args<A_COUNT> a("paged_attention", attention_names, A_SCALE, args, nargs, kwnames);
+        require("paged_attention", attention_names, a, {A_Q, A_KC, A_VC, A_TABLE, A_CU, A_LEN, A_MAXNEW, A_MAXLEN});
+        const at::Tensor &q = tensor(a.v[A_Q], "q"), &table = tensor(a.v[A_TABLE], "table");
+        const Cache c = cache(a.v[A_KC], a.v[A_VC]);
+        const auto* tp = (const int32_t*)matrix(table, "table");
+        ciar_attention_params p = attention_params(q, c, table, a.v[A_MAXNEW], a.v[A_MAXLEN]);
+        if (a.given(A_SCALE)) p.scale = (float)number(a.v[A_SCALE], "scale");
+        const int64_t T = q.size(0), Hq = q.size(1), R = table.size(0);
+        const void* qp = head_rows(q, "q", at::kBFloat16, T, Hq, c.dim);
+        const auto* cu = (const int32_t*)list(a.v[A_CU], "cu_new", at::kInt, R + 1);
+        const auto* len = (const int32_t*)list(a.v[A_LEN], "kv_len", at::kInt, R);
+        Outputs o(a.v[A_OUT]);
+        const at::Tensor& y = o.get(s_out, "out['out']", [&] { return empty({T, Hq, c.dim}, at::kBFloat16, q); });
+        const at::Tensor& lse = o.get(s_lse, "out['lse']", [&] { return empty({T, Hq}, at::kFloat, q); });
+        void* yp = head_rows(y, "out['out']", at::kBFloat16, T, Hq, c.dim);
+        if (lse.dim() != 2 || lse.size(0) != T || lse.size(1) != Hq || lse.scalar_type() != at::kFloat || !lse.is_contiguous() || !lse.is_cuda())
+            value_error("out['lse'] must be a contiguous float32 [" + std::to_string(T) + ", " + std::to_string(Hq) + "] on the GPU");
+        p.q_stride = q.stride(0);
+        p.q_head_stride = q.stride(1);
+        p.out_stride = y.stride(0);
+        p.out_head_stride = y.stride(1);
+        at::Tensor keep;
+        size_t bytes = 0;
+        void* ws = workspace_of(a.v[A_WORKSPACE], a.given(A_WORKSPACE) ? 0 : ciar_attention_workspace_bytes(R, T, &p), q, keep, bytes);
+        void* stream = stream_of(a.v[A_STREAM]);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = ciar_paged_attention(qp, c.k, c.v, tp, cu, len, R, T, &p, yp, (float*)lse.data_ptr(), ws, bytes, stream);
+        Py_END_ALLOW_THREADS
+        check(rc);
+        return o.release();
+    });
+}
+
+enum { W_Q, W_KC, W_TABLE, W_MAXNEW, W_MAXLEN, W_COUNT };
+PyObject* attention_bytes_names[W_COUNT];
+
+PyObject* attention_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
+{
+    return guarded([&]() -> PyObject* {
+        Args<W_COUNT> a("attention_workspace_bytes", attention_bytes_names, W_COUNT, args, nargs, kwnames);
+        require("attention_workspace_bytes", attention_bytes_names, a, {W_Q, W_KC, W_TABLE, W_MAXNEW, W_MAXLEN});
+        const at::Tensor &q = tensor(a.v[W_Q], "q"), &k = tensor(a.v[W_KC], "k_cache"), &table = tensor(a.v[W_TABLE], "table");
+        if (k.dim() != 6 || table.dim() != 2) value_error("k_cache or table has the wrong number of dimensions");
+        const Cache c = {nullptr, nullptr, k.size(0), k.size(1), k.size(2) * 16, k.size(3) * 8};
+        const ciar_attention_params p = attention_params(q, c, table, a.v[W_MAXNEW], a.v[W_MAXLEN]);
+        return PyLong_FromSize_t(ciar_attention_workspace_bytes(table.size(0), q.size(0), &p));
+    });
+}
+
+enum { L_LOGITS, L_PARAMS, L_HSTART, L_HISTORY, L_PROMPT, L_DRAFTED, L_REPETITION, L_PRESENCE, L_FREQUENCY, L_BSTART, L_BIDS, L_BVALUES, L_ALLOWED,
+       L_ALLOWED_ROW, L_VOCAB, L_STREAM, L_OUT, L_WORKSPACE, L_COUNT };
+PyObject* adjust_names[L_COUNT];
+PyObject* s_left;
+
+PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
+{
+    return guarded([&]() -> PyObject* {
+        Args<L_COUNT> a("adjust_logits", adjust_names, L_HSTART, args, nargs, kwnames);
+        require("adjust_logits", adjust_names, a, {L_LOGITS, L_PARAMS});
+        const at::Tensor& x = tensor(a.v[L_LOGITS], "logits");
+        const at::ScalarType type = x.scalar_type();
+        if (type != at::kFloat && type != at::kBFloat16) type_error(std::string("logits must be float32 or bfloat16, got ") + type_name(type));
+        if (x.dim() != 2 || (x.stride(1) != 1 && x.size(1) > 1)) value_error("logits must be a 2-D tensor with unit stride along the vocabulary");
+        on_gpu(x);
+        const int64_t N = x.size(0);
+        ciar_params p;
+        ciar_params_default(&p);
+        const int64_t vocab = a.given(L_VOCAB) ? integer(a.v[L_VOCAB], "vocab") : x.size(1);
+        if (vocab < 0 || vocab > x.size(1)) value_error("vocab must be within the columns of logits");
+        p.vocab = (int32_t)std::min<int64_t>(vocab, INT32_MAX);
+        p.dtype = type == at::kFloat ? CIAR_F32 : CIAR_BF16;
+        p.row_stride = N > 1 ? x.stride(0) : std::max<int64_t>(x.stride(0), vocab);
+        PyObject* window = PyObject_GetAttr(a.v[L_PARAMS], s_window);
+        if (!window) pending();
+        const int64_t K = integer(window, "params.window");
+        Py_DECREF(window);
+        p.window = (int32_t)std::min<int64_t>(std::max<int64_t>(K, 0), INT32_MAX);
+        const int64_t W = K > 0 ? (N + K - 1) / K : 0;
+        ciar_adjustments j = {};
+        j.struct_size = sizeof j;
+        auto per = [&](int i, const char* name, at::ScalarType t, int64_t n) -> void* { return a.given(i) ? list(a.v[i], name, t, n) : nullptr; };
+        j.history_start = (const int64_t*)per(L_HSTART, "history_start", at::kLong, W + 1);
+        j.history = (const int32_t*)per(L_HISTORY, "history", at::kInt, -1);
+        j.history_len = j.history || a.given(L_HISTORY) ? tensor(a.v[L_HISTORY], "history").numel() : 0;
+        j.prompt_len = (const int32_t*)per(L_PROMPT, "prompt_len", at::kInt, W);
+        j.drafted = (const int32_t*)per(L_DRAFTED, "drafted", at::kInt, N);
+        j.repetition = (const float*)per(L_REPETITION, "repetition", at::kFloat, W);
+        j.presence = (const float*)per(L_PRESENCE, "presence", at::kFloat, W);
+        j.frequency = (const float*)per(L_FREQUENCY, "frequency", at::kFloat, W);
+        j.bias_start = (const int64_t*)per(L_BSTART, "bias_start", at::kLong, W + 1);
+        j.bias_ids = (const int32_t*)per(L_BIDS, "bias_ids", at::kInt, -1);
+        j.bias_len = a.given(L_BIDS) ? tensor(a.v[L_BIDS], "bias_ids").numel() : 0;
+        j.bias_values = (const float*)per(L_BVALUES, "bias_values", at::kFloat, j.bias_len);
+        // (an empty list has no address: nothing lies in it)
+        if (a.given(L_HISTORY) && j.history_len == 0) { j.history = nullptr; j.history_start = nullptr; j.prompt_len = nullptr; }
+        if (a.given(L_BIDS) && j.bias_len == 0) { j.bias_ids = nullptr; j.bias_start = nullptr; j.bias_values = nullptr; }
+        if (a.given(L_ALLOWED)) {
+            const at::Tensor& m = tensor(a.v[L_ALLOWED], "allowed");
+            j.allowed = (const int32_t*)matrix(m, "allowed");
+            if (m.size(1) * 32 < vocab) value_error("allowed must have " + std::to_string((vocab + 31) / 32) + " words a row, got " + std::to_string(m.size(1)));
+            j.mask_rows = (int32_t)std::min<int64_t>(m.size(0), INT32_MAX);
+            j.allowed_stride = row_stride(m);
+        }
+        j.allowed_row = (const int32_t*)per(L_ALLOWED_ROW, "allowed_row", at::kInt, N);
+        Outputs o(a.v[L_OUT]);
+        // (rows laid out like the input's: a padded row stays readable and aligned)
+        const at::Tensor& y = o.get(adjust_names[L_LOGITS], "out['logits']", [&] { return empty({N, p.row_stride}, type, x).narrow(1, 0, vocab); });
+        if (y.scalar_type() != type || y.dim() != 2 || y.size(0) != N || y.size(1) < vocab || (y.stride(1) != 1 && y.size(1) > 1) || !y.is_cuda())
+            value_error("out['logits'] must match logits in dtype and rows, with unit stride along the vocabulary");
+        auto* left = (int32_t*)list(o.get(s_left, "out['left']", [&] { return empty({N}, at::kInt, x); }), "out['left']", at::kInt, N);
+        at::Tensor keep;
+        size_t bytes = 0;
+        void* ws = workspace_of(a.v[L_WORKSPACE], a.given(L_WORKSPACE) ? 0 : ciar_adjust_workspace_bytes(N, &p), x, keep, bytes);
+        void* stream = stream_of(a.v[L_STREAM]);
+        const int64_t stride = N > 1 ? y.stride(0) : std::max<int64_t>(y.stride(0), vocab);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = ciar_adjust_logits(x.data_ptr(), N, &p, &j, y.data_ptr(), stride, left, ws, bytes, stream);
+        Py_END_ALLOW_THREADS
+        check(rc);
+        return o.release();
+    });
+}
+
+#define CIAR_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL | METH_KEYWORDS
+
+PyMethodDef methods[] = {
+    {"cache_plan", CIAR_FAST(cache_plan),
+     "cache_plan(lengths, new, held, ring, ring_state, table, tokens, *, page_size, kept=None, stream=None, out=None) -> dict\n--\n\n"
+     "``ciar_cache_plan``: pages, slots and positions of the next new tokens of every request; ``table`` and ``ring`` are\n"
+     "updated in place.  ``lengths``, ``new``, ``held``, ``kept`` int32 [R], ``ring`` int32 [pages], ``ring_state`` int64 [2],\n"
+     "``table`` int32 [R, width]; ``tokens``: places for new tokens in this step.  Returns lengths, kv_len, held int32 [R],\n"
+     "cu_new int32 [R + 1], granted uint8 [R], ring_state int64 [2] and slots, positions, requests int32 [tokens]; ``out`` may\n"
+     "carry preallocated tensors under the same names."},
+    {"rotary", CIAR_FAST(rotary),
+     "rotary(q, k, positions, inv_freq, *, layout='half', inverse=False, magnitude=1.0, v=None, k_cache=None, v_cache=None, slots=None, stream=None, out=None) -> dict\n--\n\n"
+     "``ciar_rotary``: ``q`` [T, heads, D] and ``k`` [T, kv_heads, D] (float32 or bfloat16, any strides between tokens and\n"
+     "heads) turned by ``positions`` int32 [T] times ``inv_freq`` float64 [n / 2], the first n dimensions of a head.  ``layout``:\n"
+     "'half' pairs dimension p with p + n / 2, 'interleaved' 2 p with 2 p + 1.  ``inverse`` turns back, which is the gradient:\n"
+     "of the turned tensors' gradients it makes those of q and k.  With ``v``, ``k_cache``, ``v_cache`` and ``slots`` int32 [T]\n"
+     "(bfloat16) the turned keys and the values go into the cache.  Returns q, and k without a cache; ``out`` may carry them."},
+    {"paged_attention", CIAR_FAST(paged_attention),
+     "paged_attention(q, k_cache, v_cache, table, cu_new, kv_len, max_new, max_len, *, scale=None, stream=None, out=None, workspace=None) -> dict\n--\n\n"
+     "``ciar_paged_attention``: the new tokens ``q`` [T, heads, D] (bfloat16) of R requests over the cache.  ``table`` int32\n"
+     "[R, width], ``cu_new`` int32 [R + 1], ``kv_len`` int32 [R]; no request has more than ``max_new`` new tokens and\n"
+     "``max_len`` tokens in the cache.  ``scale`` defaults to 1 / sqrt(D).  Returns out [T, heads, D] bfloat16 and lse\n"
+     "[T, heads] float32; ``out`` may carry them."},
+    {"attention_workspace_bytes", CIAR_FAST(attention_workspace_bytes),
+     "attention_workspace_bytes(q, k_cache, table, max_new, max_len) -> int\n--\n\nBytes of workspace ``paged_attention`` asks for (0: none)."},
+    {"adjust_logits", CIAR_FAST(adjust_logits),
+     "adjust_logits(logits, params, *, history_start=None, history=None, prompt_len=None, drafted=None, repetition=None, presence=None, frequency=None, "
+     "bias_start=None, bias_ids=None, bias_values=None, allowed=None, allowed_row=None, vocab=None, stream=None, out=None, workspace=None) -> dict\n--\n\n"
+     "``ciar_adjust_logits``: penalties, biases and grammar masks on the rows of ``logits``, ``params.window`` rows to a request.\n"
+     "``history`` int32 with ``history_start`` int64 [W + 1] (its offsets), ``prompt_len`` int32 [W], ``drafted`` int32 [N],\n"
+     "``repetition`` / ``presence`` / ``frequency`` float32 [W]; ``bias_ids`` int32 ascending and ``bias_values`` float32 with\n"
+     "``bias_start`` int64 [W + 1]; ``allowed`` int32 [masks, words] bits with ``allowed_row`` int32 [N] (negative: no mask).  Each\n"
+     "group may be left out.  Returns logits (``out['logits']`` may be ``logits`` itself) and left int32 [N], the finite logits left\n"
+     "in each row."},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_step", "The verification step's operators (see step.py).", -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+bool intern(PyObject** to, std::initializer_list<const char*> names)
+{
+    for (const char* n : names)
+        if (!(*to++ = PyUnicode_InternFromString(n))) return false;
+    return true;
+}
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__step()
+{
+    if (!intern(plan_names, {"lengths", "new", "held", "ring", "ring_state", "table", "tokens", "page_size", "kept", "stream", "out"}) ||
+        !intern(plan_outputs, {"lengths", "kv_len", "cu_new", "held", "granted", "ring_state", "slots", "positions", "requests"}) ||
+        !intern(rotary_names, {"q", "k", "positions", "inv_freq", "layout", "inverse", "magnitude", "v", "k_cache", "v_cache", "slots", "stream", "out"}) ||
+        !intern(attention_names, {"q", "k_cache", "v_cache", "table", "cu_new", "kv_len", "max_new", "max_len", "scale", "stream", "out", "workspace"}) ||
+        !intern(attention_bytes_names, {"q", "k_cache", "table", "max_new", "max_len"}) ||
+        !intern(adjust_names, {"logits", "params", "history_start", "history", "prompt_len", "drafted", "repetition", "presence", "frequency",
+                               "bias_start", "bias_ids", "bias_values", "allowed", "allowed_row", "vocab", "stream", "out", "workspace"}) ||
+        !intern(&s_window, {"window"}) || !intern(&s_cuda_stream, {"cuda_stream"}) || !intern(&s_half, {"half"}) ||
+        !intern(&s_interleaved, {"interleaved"}) || !intern(&s_out, {"out"}) || !intern(&s_lse, {"lse"}) || !intern(&s_left, {"left"}))
+        return nullptr;
+    return PyModule_Create(&module);
+}
