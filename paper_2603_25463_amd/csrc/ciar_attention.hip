@@ -56,12 +56,13 @@ __device__ __forceinline__ void add_acc(V& acc, const V& y, bool take)
     __builtin_amdgcn_sched_barrier(0);
 }
 
-__device__ __forceinline__ bool not_finite(u32x4 v)                 // any of eight bfloat16 values
+// Whether any of eight bfloat16 values is not finite, as bits 15 and 31 of the result (an exponent of ones, plus one).
+__device__ __forceinline__ uint32_t not_finite(u32x4 v)
 {
-    bool bad = false;
+    uint32_t any = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) bad |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
-    return bad;
+    for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7f807f80u) + 0x00800080u;
+    return any & 0x80008000u;
 }
 // Eight consecutive tokens' values of one dimension, the first of them token `t`: those from `end` on as zeros, and of the others
 // the finite ones (the rest as zeros), or with `other` the rest (and zeros).
@@ -292,15 +293,20 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
                 n0 = atom_at(2 * (step + 8)); n1 = atom_at(2 * (step + 8) + 1);
                 if (t0 + kSteps > least) {
                     // Where rows see different tokens, a value that is not finite must not reach those that do not see it (0 * inf):
-                    // it is left out here.
+                    // it is left out here.  (Finite ones meet weights of zero.)
                     hide(t0);
+                    uint32_t any = 0;
 #pragma unroll
-                    for (int b = 0; b < D / 16; ++b) {
-                        const u32x4 x = __builtin_bit_cast(u32x4, v[b]);
-                        const u32x4 y = cleaned(x, t0 + 8 * grp, most, false);
+                    for (int b = 0; b < D / 16; ++b) any |= not_finite(__builtin_bit_cast(u32x4, v[b]));
+                    if (__any(any != 0)) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) odd |= t0 + 8 * grp + e < most && (x[e / 2] ^ y[e / 2]) & (e & 1 ? 0xffff0000u : 0xffffu);
-                        v[b] = __builtin_bit_cast(bf16x8, y);
+                        for (int b = 0; b < D / 16; ++b) {
+                            const u32x4 x = __builtin_bit_cast(u32x4, v[b]);
+                            const u32x4 y = cleaned(x, t0 + 8 * grp, most, false);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) odd |= t0 + 8 * grp + e < most && (x[e / 2] ^ y[e / 2]) & (e & 1 ? 0xffff0000u : 0xffffu);
+                            v[b] = __builtin_bit_cast(bf16x8, y);
+                        }
                     }
                 }
                 bf16x8 w[RT];
@@ -709,18 +715,28 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
                     }
                     total[i] += sum;
                 }
-                // values that no row sees are zeros; one that is not finite must not reach the rows that do not see it (0 * inf): left out
+                // A value that is not finite must not reach the rows that do not see it (0 * inf): left out.  (Finite ones meet weights of
+                // zero.)
+                uint32_t any = 0;
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) any |= not_finite(__builtin_bit_cast(u32x4, value(slot, a, b)));
+                const bool clean = __any(any != 0);
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int b = 0; b < DB; ++b) {
                         const int t = t0 + a * kAtom + 8 * half;
-                        const u32x4 y = __builtin_bit_cast(u32x4, value(slot, a, b)), z = cleaned(y, t, most, false);
+                        u32x4 z = __builtin_bit_cast(u32x4, value(slot, a, b));
+                        if (clean) {
+                            const u32x4 y = z;
+                            z = cleaned(y, t, most, false);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) odd |= t + e < most && (y[e / 2] ^ z[e / 2]) & (e & 1 ? 0xffff0000u : 0xffffu);
+                            for (int e = 0; e < 8; ++e) odd |= t + e < most && (y[e / 2] ^ z[e / 2]) & (e & 1 ? 0xffff0000u : 0xffffu);
+                        }
 #pragma unroll
                         for (int i = 0; i < QT; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), wa.at(i, a), acc[i][b], 0, 0, 0);
-                        __builtin_amdgcn_sched_barrier(0);
                     }
             }
             slot = slot + 1 == SLOTS ? 0 : slot + 1;
