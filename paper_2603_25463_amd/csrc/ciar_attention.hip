@@ -916,38 +916,49 @@ struct Shape {
 };
 constexpr int kJoinFew = 8;                                        // parts that join_kernel takes one after another
 
-Shape shape_of(const AttentionArgs& a)
+// A kind of shape and what it takes, in us, with what the kernels measured.  Workgroups run in rounds of as many as the compute units
+// hold; a part costs its steps, a start and an end, and parts cost the launch that joins them, and the writing and reading of their
+// rows.  Few rows: 0.65 us a step of four waves at 128 dimensions while memory keeps up (5.5 TB/s over all) and 5 us a workgroup; many
+// rows: 3.4 TFLOP/s a unit and 15 us; joining: 6 us and 4 TB/s.  (Windows of 8 tokens, 32 requests, 128 units of 64 rows over 4100
+// tokens: 1 part 69 us, 2 parts 54.6; one token, 2 units over 200001: 64 parts 56.6 us, 128 parts 42.7; one token, 512 units over
+// 4096: 1 part 140 us, 2 parts 149.)
+double cost_of(const AttentionArgs& a, bool many, int rows_each, Shape* s)
 {
-    Shape s;
     const int64_t rows = (int64_t)a.max_new * (a.q_heads / a.kv_heads);
-    // (one block of few_rows_kernel: the rows whose queries and outputs a wave's registers hold)
-    s.many = rows > (a.D <= 128 ? 64 : a.D <= 192 ? 32 : 16);
-    if (s.many) s.rows = a.D <= 128 && rows > 128 ? 256 : 128;
-    else s.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-    s.blocks = (int)((rows + s.rows - 1) / s.rows);
-    if (s.blocks < 1) s.blocks = 1;
-    // Parts: workgroups run in rounds of as many as the compute units hold; a part costs its steps, a start and an end, and parts cost
-    // the launch that joins them, and the writing and reading of their rows.  In us, with what the kernels measured: few rows, 0.65 us
-    // a step of four waves at 128 dimensions while memory keeps up (5.5 TB/s over all) and 5 us a workgroup; many rows, 3.4 TFLOP/s a
-    // unit and 8 us; joining, 6 us and 4 TB/s.  (Windows of 8 tokens, 32 requests, 128 units of 64 rows over 4100 tokens: 1 part 69 us, 2
-    // parts 54.6; one token, 2 units over 200001: 64 parts 56.6 us, 128 parts 42.7; one token, 512 units over 4096: 1 part 140 us, 2
-    // parts 149.)
-    const int64_t units = (int64_t)a.R * a.kv_heads * s.blocks;
-    const int per_unit = s.many ? 1 : s.rows * a.D <= 16 * 64 ? 3 : s.rows * a.D <= 16 * 128 ? 2 : 1;
+    s->many = many;
+    s->rows = rows_each;
+    s->blocks = (int)((rows + rows_each - 1) / rows_each);
+    if (s->blocks < 1) s->blocks = 1;
+    const int64_t units = (int64_t)a.R * a.kv_heads * s->blocks;
+    const int per_unit = many ? 1 : rows_each * a.D <= 16 * 64 ? 3 : rows_each * a.D <= 16 * 128 ? 2 : 1;
     const int64_t resident = (int64_t)compute_units() * per_unit;
-    const double step_us = s.many ? 4.0 * kSteps * s.rows * a.D / 3.4e6 : 0.65 * a.D / 128;
+    const double step_us = many ? 4.0 * kSteps * rows_each * a.D / 3.4e6 : 0.65 * a.D / 128, wg_us = many ? 15.0 : 5.0;
     const int64_t steps = ((int64_t)a.max_len + kSteps - 1) / kSteps;
-    const double memory_us = s.many ? 0.0 : (double)units * steps * (4 * kSteps * a.D) / 5.5e6;
+    const double memory_us = many ? 0.0 : (double)units * steps * (4 * kSteps * a.D) / 5.5e6;
     const double row_us = (double)a.T * a.q_heads * (a.D * 8 + 16) / 4e6;
-    s.splits = 1;
+    s->splits = 1;
     double best = 0.0;
     for (int64_t n = 1; n <= 256 && n <= (steps + 3) / 4; n += n < 16 ? 1 : n < 64 ? 4 : 16) {
         const int64_t rounds = (units * n + resident - 1) / resident, each = (steps + n - 1) / n;
-        const double own = (double)rounds * ((double)each * step_us + (s.many ? 8.0 : 5.0));
-        const double us = (own > memory_us + 5.0 ? own : memory_us + 5.0) + (n > 1 ? 6.0 + (double)n * row_us : 0.0);
-        if (n == 1 || us < 0.95 * best) { best = us; s.splits = (int)n; }
+        const double own = (double)rounds * ((double)each * step_us + wg_us), least = memory_us + wg_us;
+        const double us = (own > least ? own : least) + (n > 1 ? 6.0 + (double)n * row_us : 0.0);
+        if (n == 1 || us < 0.95 * best) { best = us; s->splits = (int)n; }
     }
-    return s;
+    return best;
+}
+
+Shape shape_of(const AttentionArgs& a)
+{
+    const int64_t rows = (int64_t)a.max_new * (a.q_heads / a.kv_heads);
+    // few_rows_kernel: up to the rows whose queries and outputs a wave's registers hold, in one block or (short contexts) several;
+    // many_rows_kernel: more rows than one such block.  (256 rows, 8 heads: over 128 tokens 15.3 us against 20.5, over 2048 tokens
+    // 26.7 against 33.)
+    const int widest = a.D <= 128 ? 64 : a.D <= 192 ? 32 : 16;
+    Shape few, many;
+    const double few_us = cost_of(a, false, rows <= 16 ? 16 : rows <= 32 || widest < 32 ? (widest < 32 ? 16 : 32) : widest, &few);
+    if (rows <= widest) return few;
+    const double many_us = cost_of(a, true, a.D <= 128 && rows > 128 ? 256 : 128, &many);
+    return few_us < many_us ? few : many;
 }
 
 template <int D, int QT>

@@ -163,10 +163,21 @@ Cache cache(PyObject* ko, PyObject* vo)
 
 // ---- outputs, stream, errors ---------------------------------------------------------------------------------------
 
+// A tensor that was allocated here, in the order of the current stream, and is used on another: its memory is not handed on before
+// that stream is through with it.
+void record(PyObject* tensor, PyObject* stream)
+{
+    if (!stream || stream == Py_None) return;
+    PyObject* r = PyObject_CallMethod(tensor, "record_stream", "O", stream);
+    if (!r) pending();
+    Py_DECREF(r);
+}
+
 // The dictionary that a call returns: a copy of what `out` brings, completed by what it does not.
 struct Outputs {
     PyObject* dict;
-    explicit Outputs(PyObject* out)
+    PyObject* stream;                                               // of the call, if not the current one
+    Outputs(PyObject* out, PyObject* on) : stream(on && on != Py_None ? on : nullptr)
     {
         if (out && out != Py_None && !PyDict_Check(out)) type_error("out must be a dict");
         dict = out && out != Py_None ? PyDict_Copy(out) : PyDict_New();
@@ -189,6 +200,7 @@ struct Outputs {
             const int rc = PyDict_SetItem(dict, name, o);
             Py_DECREF(o);                                           // (the dictionary holds it)
             if (rc != 0) pending();
+            record(o, stream);
         }
         return tensor(o, what);
     }
@@ -219,7 +231,7 @@ void* stream_of(PyObject* o)
 }
 
 // The caller's workspace, or a fresh one of `need` bytes (held by `keep`; the allocator reuses it in the order of the stream).
-void* workspace_of(PyObject* o, size_t need, const at::Tensor& like, at::Tensor& keep, size_t& bytes)
+void* workspace_of(PyObject* o, size_t need, const at::Tensor& like, PyObject* stream, at::Tensor& keep, size_t& bytes)
 {
     if (o && o != Py_None) {
         const at::Tensor& t = tensor(o, "workspace");
@@ -230,6 +242,12 @@ void* workspace_of(PyObject* o, size_t need, const at::Tensor& like, at::Tensor&
     bytes = need;
     if (!need) return nullptr;
     keep = empty({(int64_t)need}, at::kByte, like);
+    if (stream && stream != Py_None) {
+        PyObject* t = THPVariable_Wrap(keep);
+        if (!t) pending();
+        record(t, stream);
+        Py_DECREF(t);
+    }
     return keep.data_ptr();
 }
 
@@ -289,7 +307,7 @@ PyObject* cache_plan(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObjec
         static const struct { const char* name; at::ScalarType type; } what[PO_COUNT] = {
             {"out['lengths']", at::kInt}, {"out['kv_len']", at::kInt}, {"out['cu_new']", at::kInt}, {"out['held']", at::kInt}, {"out['granted']", at::kByte},
             {"out['ring_state']", at::kLong}, {"out['slots']", at::kInt}, {"out['positions']", at::kInt}, {"out['requests']", at::kInt}};
-        Outputs o(a.v[P_OUT]);
+        Outputs o(a.v[P_OUT], a.v[P_STREAM]);
         void* p[PO_COUNT];
         for (int i = 0; i < PO_COUNT; ++i) {
             const int64_t n = i == PO_CU ? R + 1 : i == PO_STATE ? 2 : i >= PO_SLOTS ? T : R;
@@ -345,7 +363,7 @@ PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* k
         const auto* fp = (const double*)list(freq, "inv_freq", at::kDouble, -1);
         if (freq.numel() > INT32_MAX / 2) value_error("inv_freq is too long");
         p.rotary_dim = (int32_t)(2 * freq.numel());
-        Outputs o(a.v[R_OUT]);
+        Outputs o(a.v[R_OUT], a.v[R_STREAM]);
         const at::Tensor& qo = o.get(rotary_names[R_Q], "out['q']", [&] { return empty({T, Hq, D}, type, q); });
         void *qop = head_rows(qo, "out['q']", type, T, Hq, D), *kop = nullptr;
         Cache c = {};
@@ -424,7 +442,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs, Py
         const void* qp = head_rows(q, "q", at::kBFloat16, T, Hq, c.dim);
         const auto* cu = (const int32_t*)list(a.v[A_CU], "cu_new", at::kInt, R + 1);
         const auto* len = (const int32_t*)list(a.v[A_LEN], "kv_len", at::kInt, R);
-        Outputs o(a.v[A_OUT]);
+        Outputs o(a.v[A_OUT], a.v[A_STREAM]);
         const at::Tensor& y = o.get(s_out, "out['out']", [&] { return empty({T, Hq, c.dim}, at::kBFloat16, q); });
         const at::Tensor& lse = o.get(s_lse, "out['lse']", [&] { return empty({T, Hq}, at::kFloat, q); });
         void* yp = head_rows(y, "out['out']", at::kBFloat16, T, Hq, c.dim);
@@ -436,7 +454,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs, Py
         p.out_head_stride = y.stride(1);
         at::Tensor keep;
         size_t bytes = 0;
-        void* ws = workspace_of(a.v[A_WORKSPACE], a.given(A_WORKSPACE) ? 0 : ciar_attention_workspace_bytes(R, T, &p), q, keep, bytes);
+        void* ws = workspace_of(a.v[A_WORKSPACE], a.given(A_WORKSPACE) ? 0 : ciar_attention_workspace_bytes(R, T, &p), q, a.v[A_STREAM], keep, bytes);
         void* stream = stream_of(a.v[A_STREAM]);
         int rc;
         Py_BEGIN_ALLOW_THREADS
@@ -518,7 +536,7 @@ PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
             j.allowed_stride = row_stride(m);
         }
         j.allowed_row = (const int32_t*)per(L_ALLOWED_ROW, "allowed_row", at::kInt, N);
-        Outputs o(a.v[L_OUT]);
+        Outputs o(a.v[L_OUT], a.v[L_STREAM]);
         // (rows laid out like the input's: a padded row stays readable and aligned)
         const at::Tensor& y = o.get(adjust_names[L_LOGITS], "out['logits']", [&] { return empty({N, p.row_stride}, type, x).narrow(1, 0, vocab); });
         if (y.scalar_type() != type || y.dim() != 2 || y.size(0) != N || y.size(1) < vocab || (y.stride(1) != 1 && y.size(1) > 1) || !y.is_cuda())
@@ -526,7 +544,7 @@ PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
         auto* left = (int32_t*)list(o.get(s_left, "out['left']", [&] { return empty({N}, at::kInt, x); }), "out['left']", at::kInt, N);
         at::Tensor keep;
         size_t bytes = 0;
-        void* ws = workspace_of(a.v[L_WORKSPACE], a.given(L_WORKSPACE) ? 0 : ciar_adjust_workspace_bytes(N, &p), x, keep, bytes);
+        void* ws = workspace_of(a.v[L_WORKSPACE], a.given(L_WORKSPACE) ? 0 : ciar_adjust_workspace_bytes(N, &p), x, a.v[L_STREAM], keep, bytes);
         void* stream = stream_of(a.v[L_STREAM]);
         const int64_t stride = N > 1 ? y.stride(0) : std::max<int64_t>(y.stride(0), vocab);
         int rc;

@@ -630,6 +630,28 @@ def test_step_twice_and_on_another_stream(ciar):
         assert torch.equal(a[k], b[k]) and torch.equal(a[k], c[k]), k
 
 
+def test_calls_on_a_given_stream(ciar):
+    """A stream handed to the calls: outputs and workspaces that they allocate stay theirs until that stream is through."""
+    say("[step] given stream")
+    lens, news, Hq, Hk, D = [9000, 5000], [1, 1], 8, 2, 128
+    kc, vc, table, kv = make_cache(ciar, lens, Hk, D, 16, seed=5)
+    q = torch.randn((2, Hq, D), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    x, a = adjust_case(40, 5000, 40, torch.bfloat16, 3, ALL)
+    x, a = x.cuda(), {k: v.cuda() for k, v in a.items()}
+    cu, kl = i32([0, 1, 2]), i32(lens)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)                                # the calls below wait for this
+    o = ciar.paged_attention(q, kc, vc, table, cu, kl, 1, 9000, stream=side)
+    y = ciar.adjust_logits(x, ciar.Params(window=40), stream=side, **a)
+    trash = [torch.full((1 << 18,), 255, dtype=torch.uint8, device="cuda") for _ in range(32)]      # on the current stream, at once
+    torch.cuda.synchronize()
+    check_attention(o, q.cpu(), kv, news, [0, 1], 1 / math.sqrt(D), Hq // Hk)
+    check_adjust(y, x.cpu(), 40, a)
+    del trash
+
+
 def test_step_in_a_graph(ciar):
     """Captured once, replayed on new inputs several times, with eager steps between the replays."""
     say("[step] graph")
