@@ -1,0 +1,23 @@
+"""The host code of the verification step's C ABI (csrc/ciar_step.cpp, with ciar_api.cpp's error text) under AddressSanitizer +
+UndefinedBehaviorSanitizer and under ThreadSanitizer, with the stand-in launchers of tests/sanitize/step_driver.cpp (CPU only)."""
+import os
+import subprocess
+
+import pytest
+
+from test_sanitizers import API, AS_PLAIN_CXX, CLANG, ROOT, SAN, _run
+
+STEP = os.path.join(ROOT, "paper_2603_25463_amd", "csrc", "ciar_step.cpp")
+
+
+@pytest.mark.parametrize("sanitize", ["address,undefined", "thread"])
+def test_step_host_code_under_sanitizers(tmp_path, sanitize):
+    if not os.path.exists(CLANG):
+        pytest.skip("ROCm's clang++ is not installed")
+    exe = str(tmp_path / "step_san")
+    cmd = [CLANG, "-O1", "-g", "-std=c++17", *AS_PLAIN_CXX, f"-fsanitize={sanitize}", "-fno-omit-frame-pointer"]
+    if sanitize != "thread":
+        cmd.append("-fno-sanitize-recover=all")
+    cmd += [API, STEP, os.path.join(SAN, "api_stubs.cpp"), os.path.join(SAN, "step_driver.cpp"), "-o", exe, "-lpthread"]
+    subprocess.run(cmd, check=True)
+    _run(exe, TSAN_OPTIONS="halt_on_error=1 exitcode=66", ASAN_OPTIONS="detect_leaks=1")
