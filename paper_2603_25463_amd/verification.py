@@ -1,0 +1,114 @@
+"""A verification loop over the operators of ``step``: drafted windows of image tokens, a one-layer verifier with a paged cache, the
+accept test.  Random weights: it shows how the calls fit together, and nothing in a step waits for the GPU.
+
+    python -m paper_2603_25463_amd.verification [--requests 8] [--window 8] [--steps 16]
+
+A step of R requests and windows of K: the drafter draws K tokens behind each request's last one; the verifier takes the last token
+and the first K - 1 drafted ones as its new tokens, so that its row j holds the distribution that drafted token j is tested against.
+Row j's accepted prefix is a tokens long: the cache keeps the last token and the accepted ones that went in, min(a + 1, K), the next
+plan's ``kept``; the next last token is the replacement, or the last drafted token of a window that was accepted throughout.
+"""
+from __future__ import annotations
+
+import argparse
+
+import torch
+
+from .binding import Params, verify
+from .step import adjust_logits, cache_plan, cache_shapes, paged_attention, rotary
+
+
+class VerificationLoop:
+    def __init__(self, requests: int = 8, window: int = 8, vocab: int = 1024, heads: int = 8, kv_heads: int = 2, head_dim: int = 64,
+                 page_size: int = 16, max_len: int = 512, seed: int = 0, device="cuda"):
+        self.R, self.K, self.V, self.Hq, self.Hk, self.D = requests, window, vocab, heads, kv_heads, head_dim
+        self.page, self.max_len, self.dev = page_size, max_len, torch.device(device)
+        self.gen = torch.Generator(device=self.dev).manual_seed(seed)
+        R, K, width, E = requests, window, -(-(max_len + window) // page_size), heads * head_dim
+        rnd = lambda *s, scale=1.0: (torch.randn(s, generator=self.gen, device=self.dev) * scale).bfloat16()
+        self.embed, self.w_qkv = rnd(vocab, E), rnd(E, (heads + 2 * kv_heads) * head_dim, scale=E ** -0.5)
+        self.w_out, self.w_logits = rnd(E, E, scale=E ** -0.5), rnd(E, vocab, scale=1.5 * E ** -0.5)
+        self.inv_freq = 10000.0 ** (-torch.arange(head_dim // 2, dtype=torch.float64, device=self.dev) / (head_dim // 2))
+        pages = R * width
+        ks, vs = cache_shapes(pages, kv_heads, head_dim, page_size)
+        self.k_cache, self.v_cache = (torch.zeros(s, dtype=torch.bfloat16, device=self.dev) for s in (ks, vs))
+        i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=self.dev)
+        self.table, self.ring = i32(R, width), torch.arange(pages, dtype=torch.int32, device=self.dev)
+        self.ring_state = torch.tensor([0, pages], device=self.dev)
+        self.lengths, self.held, self.kept, self.new = i32(R), i32(R), i32(R), i32(R) + K
+        # what each request has said, unused places -1 (no token): one list for the penalties
+        self.said = torch.full((R, max_len + K + 1), -1, dtype=torch.int32, device=self.dev)
+        self.count = torch.ones(R, dtype=torch.int64, device=self.dev)
+        self.last = torch.randint(0, vocab, (R,), generator=self.gen, device=self.dev, dtype=torch.int32)
+        self.said[:, 0] = self.last
+        self.history_start = torch.arange(R + 1, device=self.dev) * self.said.shape[1]
+        self.penalty = {"repetition": torch.full((R,), 1.1, device=self.dev), "presence": torch.full((R,), 0.1, device=self.dev),
+                        "frequency": torch.full((R,), 0.05, device=self.dev)}
+        # one grammar state: a sixteenth of the tokens is never allowed
+        words = torch.full((1, -(-vocab // 32)), -1, dtype=torch.int32, device=self.dev)
+        self.allowed = words & ~0x00010001
+        self.allowed_row = i32(R * K)
+        self.params = Params(window=K)
+
+    def _uniform(self, n: int):
+        return torch.rand(n, generator=self.gen, device=self.dev).clamp(max=1.0 - 2.0 ** -24)
+
+    def draft(self):
+        """K tokens behind every request's last one, each from the embedding of the one before it: (ids [R K], logits [R K, V])."""
+        ids, rows, token = [], [], self.last
+        for _ in range(self.K):
+            logits = (self.embed[token.long()] @ self.w_logits).float()
+            noise = -torch.log(-torch.log(self._uniform(self.R * self.V).clamp(min=1e-9).view(self.R, self.V)))
+            token = (logits + noise).argmax(1).int()
+            ids.append(token)
+            rows.append(logits)
+        return torch.stack(ids, 1).reshape(-1).contiguous(), torch.stack(rows, 1).reshape(self.R * self.K, self.V).contiguous()
+
+    def verifier(self, tokens):
+        """Logits of the new tokens [R K] behind what the cache holds; their keys and values go into the cache."""
+        T = tokens.numel()
+        plan = cache_plan(self.lengths, self.new, self.held, self.ring, self.ring_state, self.table, T, page_size=self.page,
+                          kept=self.kept)
+        x = self.embed[tokens.long()]
+        qkv = (x @ self.w_qkv).view(T, self.Hq + 2 * self.Hk, self.D)
+        q, k, v = qkv.split([self.Hq, self.Hk, self.Hk], 1)
+        q = rotary(q, k, plan["positions"], self.inv_freq, v=v, k_cache=self.k_cache, v_cache=self.v_cache, slots=plan["slots"])["q"]
+        y = paged_attention(q, self.k_cache, self.v_cache, self.table, plan["cu_new"], plan["kv_len"], self.K, self.max_len + self.K)
+        h = x + y["out"].view(T, -1) @ self.w_out
+        self.lengths, self.held, self.ring_state, self.plan = plan["lengths"], plan["held"], plan["ring_state"], plan
+        return (h @ self.w_logits).float()
+
+    def step(self) -> dict:
+        R, K = self.R, self.K
+        ids, draft = self.draft()
+        window = ids.view(R, K)
+        logits = self.verifier(torch.cat([self.last[:, None], window[:, :-1]], 1).reshape(-1))
+        adjusted = adjust_logits(logits, self.params, history_start=self.history_start, history=self.said.view(-1), drafted=ids,
+                                 allowed=self.allowed, allowed_row=self.allowed_row, **self.penalty)
+        o = verify(draft, adjusted["logits"], ids, self._uniform(R * K), self._uniform(R * K), self.params)
+        accepted = o["accept_len"].long()
+        whole = accepted == K
+        self.kept = torch.clamp(o["accept_len"] + 1, max=K).int()
+        self.last = torch.where(whole, window[:, -1], o["resampled_id"]).int()
+        # what has been said now: the accepted tokens, and the replacement behind them
+        place = torch.arange(K, device=self.dev)
+        said = torch.where(place < accepted[:, None], window, torch.where(place == accepted[:, None], self.last[:, None], -1)).int()
+        self.said.scatter_(1, self.count[:, None] + place, said)
+        self.count += torch.clamp(accepted + 1, max=K)
+        return {"logits": logits, "adjusted": adjusted["logits"], "left": adjusted["left"], "draft": draft, "ids": ids, **o}
+
+
+def main() -> None:
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--requests", type=int, default=8)
+    ap.add_argument("--window", type=int, default=8)
+    ap.add_argument("--steps", type=int, default=16)
+    a = ap.parse_args()
+    loop = VerificationLoop(a.requests, a.window, max_len=a.steps * a.window + 1)
+    for i in range(a.steps):
+        o = loop.step()
+        print(f"step {i}: accepted {o['accept_len'].tolist()}, tokens in the cache {loop.plan['kv_len'].tolist()}", flush=True)
+
+
+if __name__ == "__main__":
+    main()
