@@ -918,8 +918,8 @@ constexpr int kJoinFew = 8;                                        // parts that
 
 // A kind of shape and what it takes, in us, with what the kernels measured.  Workgroups run in rounds of as many as the compute units
 // hold; a part costs its steps, a start and an end, and parts cost the launch that joins them, and the writing and reading of their
-// rows.  Few rows: 0.65 us a step of four waves at 128 dimensions while memory keeps up (5.5 TB/s over all) and 5 us a workgroup; many
-// rows: 3.4 TFLOP/s a unit and 15 us; joining: 6 us and 4 TB/s.  (Windows of 8 tokens, 32 requests, 128 units of 64 rows over 4100
+// rows.  Few rows: 0.65 us a step of four waves at 128 dimensions while memory keeps up (5.5 TB/s over all) and 6 to 12 us a workgroup (64
+// rows); many rows: 3.4 TFLOP/s a unit and 15 us; joining: 6 us and 4 TB/s.  (Windows of 8 tokens, 32 requests, 128 units of 64 rows over 4100
 // tokens: 1 part 69 us, 2 parts 54.6; one token, 2 units over 200001: 64 parts 56.6 us, 128 parts 42.7; one token, 512 units over
 // 4096: 1 part 140 us, 2 parts 149.)
 double cost_of(const AttentionArgs& a, bool many, int rows_each, Shape* s)
@@ -932,7 +932,7 @@ double cost_of(const AttentionArgs& a, bool many, int rows_each, Shape* s)
     const int64_t units = (int64_t)a.R * a.kv_heads * s->blocks;
     const int per_unit = many ? 1 : rows_each * a.D <= 16 * 64 ? 3 : rows_each * a.D <= 16 * 128 ? 2 : 1;
     const int64_t resident = (int64_t)compute_units() * per_unit;
-    const double step_us = many ? 4.0 * kSteps * rows_each * a.D / 3.4e6 : 0.65 * a.D / 128, wg_us = many ? 15.0 : 5.0;
+    const double step_us = many ? 4.0 * kSteps * rows_each * a.D / 3.4e6 : 0.65 * a.D / 128, wg_us = many ? 15.0 : rows_each == 64 ? 12.0 : 6.0;
     const int64_t steps = ((int64_t)a.max_len + kSteps - 1) / kSteps;
     const double memory_us = many ? 0.0 : (double)units * steps * (4 * kSteps * a.D) / 5.5e6;
     const double row_us = (double)a.T * a.q_heads * (a.D * 8 + 16) / 4e6;
@@ -950,15 +950,23 @@ double cost_of(const AttentionArgs& a, bool many, int rows_each, Shape* s)
 Shape shape_of(const AttentionArgs& a)
 {
     const int64_t rows = (int64_t)a.max_new * (a.q_heads / a.kv_heads);
-    // few_rows_kernel: up to the rows whose queries and outputs a wave's registers hold, in one block or (short contexts) several;
-    // many_rows_kernel: more rows than one such block.  (256 rows, 8 heads: over 128 tokens 15.3 us against 20.5, over 2048 tokens
-    // 26.7 against 33.)
+    // few_rows_kernel takes up to the rows whose queries and outputs a wave's registers hold, in one block or (each reads the keys and
+    // values) several; many_rows_kernel what is more than one block.  (us, blocks of 16, 32, 64 rows and of 256: 256 rows of 8 heads over
+    // 128 tokens 11.8, 9.9, 15.3, 19.4, over 2048 tokens 26.2, 19.9, 27.5, 31.6; 64 rows over 4096 tokens 23.8, 21.0, 28.2, 30.1; 256 rows
+    // of 32 heads over 1024 tokens 40.3, 28.3, 29.3, 36.1.)
     const int widest = a.D <= 128 ? 64 : a.D <= 192 ? 32 : 16;
-    Shape few, many;
-    const double few_us = cost_of(a, false, rows <= 16 ? 16 : rows <= 32 || widest < 32 ? (widest < 32 ? 16 : 32) : widest, &few);
-    if (rows <= widest) return few;
-    const double many_us = cost_of(a, true, a.D <= 128 && rows > 128 ? 256 : 128, &many);
-    return few_us < many_us ? few : many;
+    Shape best;
+    double best_us = cost_of(a, false, 16, &best);
+    for (int each = 32; each <= widest && each / 2 < rows; each *= 2) {
+        Shape s;
+        const double us = cost_of(a, false, each, &s);
+        if (us <= best_us) { best = s; best_us = us; }
+    }
+    if (rows > widest) {
+        Shape s;
+        if (cost_of(a, true, a.D <= 128 && rows > 128 ? 256 : 128, &s) < best_us) best = s;
+    }
+    return best;
 }
 
 template <int D, int QT>
