@@ -109,6 +109,12 @@ __device__ void fill_unclaimed(const AttentionArgs& A, int64_t from, int64_t ste
 // would otherwise all be waited for with each page.
 using table_row = const __attribute__((address_space(4))) int32_t*;
 
+// An atom of a request, as its table says: page and atom in the page.
+struct Atom {
+    int page;
+    uint32_t at;
+};
+
 // What a workgroup works on.
 struct Unit {
     int r, h, block, split;            // request, key head, block of rows, part of the tokens
@@ -202,11 +208,16 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
     const int64_t head_bytes = (int64_t)A.page * D * 2;
     const table_row row = (table_row)(A.table + (int64_t)u.r * A.table_stride);
     const int atoms = (most + kAtom - 1) / kAtom;
-    auto atom_at = [&](int atom) -> int64_t {                      // byte offset of an atom of the request
+    // An atom of the request: its page's number as the table has it (a load that is under way until the place is asked for), and its place.
+    const int64_t page_bytes = A.kv_heads * head_bytes, head_at = u.h * head_bytes;
+    auto find = [&](int atom) -> Atom {
         const uint32_t a = (uint32_t)min(atom, atoms - 1), page = __umulhi(2 * a, P.mul) >> P.shift;
-        const int p = min(max(row[page], 0), A.pages - 1);
-        return ((int64_t)p * A.kv_heads + u.h) * head_bytes + (int64_t)(a - page * P.per) * (kAtom * D * 2);
+        return {row[page], a - page * P.per};
     };
+    auto place = [&](const Atom& a) -> int64_t {                   // byte offset
+        return min(max(a.page, 0), A.pages - 1) * page_bytes + head_at + (int64_t)a.at * (kAtom * D * 2);
+    };
+    auto atom_at = [&](int atom) { return place(find(atom)); };
     // this lane's keys and values of a step
     const int koff = ((col >> 2 & 1) * 8 + (col & 3)) * 16 + grp * 256, voff = ((grp & 1) * D + col) * 16;
     bf16x8 k0[D / 32], k1[D / 32], v[D / 16];
@@ -273,7 +284,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
             int64_t a0 = atom_at(2 * step), a1 = atom_at(2 * step + 1);
             load_keys(a0, a1);
             load_values(a0, a1);
-            int64_t n0 = atom_at(2 * (step + 4)), n1 = atom_at(2 * (step + 4) + 1);
+            Atom n0 = find(2 * (step + 4)), n1 = find(2 * (step + 4) + 1);
             if (pass == 0) {
                 scores();
                 if ((step + 1) * kSteps > least) hide(step * kSteps);
@@ -288,9 +299,9 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
                 const int t0 = step * kSteps;
                 scores();
                 // the next step's keys, into the registers that have just been read (past the part's end: the last atom's again)
-                a0 = n0; a1 = n1;
+                a0 = place(n0); a1 = place(n1);
                 load_keys(a0, a1);
-                n0 = atom_at(2 * (step + 8)); n1 = atom_at(2 * (step + 8) + 1);
+                n0 = find(2 * (step + 8)); n1 = find(2 * (step + 8) + 1);
                 if (t0 + kSteps > least) {
                     // Where rows see different tokens, a value that is not finite must not reach those that do not see it (0 * inf):
                     // it is left out here.  (Finite ones meet weights of zero.)
@@ -531,11 +542,16 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
         const int64_t head_bytes = (int64_t)A.page * D * 2;
         const table_row row = (table_row)(A.table + (int64_t)u.r * A.table_stride);
         const int atoms = (most + kAtom - 1) / kAtom;
-        auto atom_at = [&](int atom) -> int64_t {
+        // An atom of the request: its page's number as the table has it (a load that is under way until the place is asked for), and its place.
+        const int64_t page_bytes = A.kv_heads * head_bytes, head_at = u.h * head_bytes;
+        auto find = [&](int atom) -> Atom {
             const uint32_t a = (uint32_t)min(atom, atoms - 1), page = __umulhi(2 * a, P.mul) >> P.shift;
-            const int p = min(max(row[page], 0), A.pages - 1);
-            return ((int64_t)p * A.kv_heads + u.h) * head_bytes + (int64_t)(a - page * P.per) * ATOM;
+            return {row[page], a - page * P.per};
         };
+        auto place = [&](const Atom& a) -> int64_t {                   // byte offset
+            return min(max(a.page, 0), A.pages - 1) * page_bytes + head_at + (int64_t)a.at * (kAtom * D * 2);
+        };
+        auto atom_at = [&](int atom) { return place(find(atom)); };
         // requests of a step whose atoms lie at a0, a1
         auto request = [&](int64_t a0, int64_t a1, int slot) {
 #pragma unroll
@@ -588,19 +604,17 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
         };
         auto hidden = [&](int t0, int i, int v) { return t0 + (v >> 3) * kAtom + 8 * half + (v & 7) >= seen[i]; };
         // the ring: step s lies in slot (s - first) % SLOTS
-        int64_t n0 = 0, n1 = 0;
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) request(atom_at(2 * (first + x)), atom_at(2 * (first + x) + 1), x);
-        n0 = atom_at(2 * (first + AHEAD));
-        n1 = atom_at(2 * (first + AHEAD) + 1);
+        Atom n0 = find(2 * (first + AHEAD)), n1 = find(2 * (first + AHEAD) + 1);
         int slot = 0, ahead = AHEAD % SLOTS;                       // of the step s of the body, and of the step that is requested in it
         // What opens step s: the steps up to s + 1 (the last AHEAD - 2 requested may be under way) have arrived, and every wave is done with s - 2
         auto open = [&](int s) {
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * MINE * (AHEAD - 2)) : "memory");
-            request(n0, n1, ahead);
+            request(place(n0), place(n1), ahead);
             ahead = ahead + 1 == SLOTS ? 0 : ahead + 1;
-            n0 = atom_at(2 * (s + AHEAD + 1));
-            n1 = atom_at(2 * (s + AHEAD + 1) + 1);
+            n0 = find(2 * (s + AHEAD + 1));
+            n1 = find(2 * (s + AHEAD + 1) + 1);
         };
         int s = first;
         Weights<QT> wa, wb;
@@ -611,12 +625,15 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
             if (pass == 0) refer(sa);
             int prev = 0;
             // The body of step s: its weights, the scores of the next step, the output of the one before (unless it is the first).
-            // Written as groups of QT matrix instructions on one operand, each followed by its share of the vector work and by the
-            // read of the operand that the group after the next one takes; nothing moves from group to group.  Two groups of the
-            // output open the body: their operands have been there since the body before, while the next step's keys are on their way.
-            constexpr int GROUPS = KS + 2 * DB, LEAD = 2;
+            // Written as groups of QT matrix instructions on one operand, with the step's vector work dealt out between them, two weights
+            // at a time: a matrix instruction runs for 32 cycles, and the next one waits for it in the way of whatever follows.  Nothing
+            // moves from slot to slot.  Operands are read from LDS a batch of groups ahead of their use, all at once behind the batch's first
+            // matrix instruction (the compiler waits for all reads that are under way, whichever it needs).  The output's first
+            // groups open the body: their operands have been there since the body before, while the next step's keys are on their way.
+            constexpr int GROUPS = KS + 2 * DB, BT = D == 32 ? 2 : 4, LEAD = BT, BATCHES = GROUPS / BT;
+            static_assert(GROUPS % BT == 0 && LEAD <= 2 * DB, "whole batches");
             constexpr int SHARE = pairs_of(16 * QT, GROUPS), SHARE1 = pairs_of(16 * QT, KS);
-            bf16x8 op[2];                                          // operands of the next two groups
+            bf16x8 op[3][BT];                                      // operands: of a body's first batch (2), of the others in turn
             auto operand = [&](int n, int keys, int values) -> bf16x8 {        // of group n
                 if (n >= LEAD && n < LEAD + KS) return key(keys, n - LEAD);
                 const int o = n < LEAD ? n : n - KS;
@@ -633,41 +650,63 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
 #pragma unroll
                     for (int v = 0; v < 16; ++v) next[i][v] = 0.f;
                 }
-                if constexpr (FIRST) { op[0] = key(after, 0); op[1] = key(after, 1); }
+                auto fetch = [&](int b) {                          // (the last batch's are the next body's first: this step's values)
 #pragma unroll
-                for (int n = FIRST ? LEAD : 0; n < GROUPS; ++n) {
-                    const bool keys = n >= LEAD && n < LEAD + KS;
-                    if (FIRST && !keys) {
-                        // (no step before: only the vector work)
-                    } else {
-                        const bf16x8 x = op[n & 1];
-                        const int o = n < LEAD ? n : n - KS;
-#pragma unroll
-                        for (int i = 0; i < QT; ++i) {
-                            if (keys) next[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][keys ? n - LEAD : 0], next[i], 0, 0, 0);
-                            else acc[i][keys ? 0 : o % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, before.at(i, keys ? 0 : o / DB), acc[i][keys ? 0 : o % DB], 0, 0, 0);
-                        }
+                    for (int k = 0; k < BT; ++k) {
+                        if (b < BATCHES) op[b & 1][k] = operand(b * BT + k, after, prev);
+                        else op[2][k] = operand(k, after, slot);
                     }
-                    // (the last two reads are the next body's first: this step's values)
-                    if (n + 2 < GROUPS) op[n & 1] = operand(n + 2, after, prev);
-                    else op[n & 1] = operand(n + 2 - GROUPS, after, slot);
-                    const int e0 = FIRST ? (n - LEAD) * SHARE1 : n * SHARE, e1 = FIRST ? e0 + SHARE1 : e0 + SHARE;
-#pragma unroll
-                    for (int e = e0; e < e1; e += 2)
-                        if (e < 16 * QT) {
-                            const int i = e / 16 < QT ? e / 16 : 0, v = e % 16;
-                            const float p0 = __builtin_amdgcn_exp2f(fmaf(now[i][v], scale, -sub[i]));
-                            const float p1 = __builtin_amdgcn_exp2f(fmaf(now[i][v + 1], scale, -sub[i]));
-                            total[i] += p0;
-                            total[i] += p1;
-                            high[i] = fmaxf(fmaxf(now[i][v], now[i][v + 1]), high[i]);
-                            w.put(i, v, p0, p1);
-                        }
-                    // (sums and maxima stay in their group, too: left to itself the compiler collects them behind the body)
+                };
+                // weights e, e + 1 of the lane's 16 QT; in two parts, or the whole
+                float x0 = 0.f, x1 = 0.f, p0 = 0.f;
+                auto weigh = [&](int e, bool begin, bool end) {
+                    if (e >= 16 * QT) return;
+                    const int i = e / 16 < QT ? e / 16 : 0, v = e % 16;
+                    if (begin) {
+                        x0 = fmaf(now[i][v], scale, -sub[i]);
+                        x1 = fmaf(now[i][v + 1], scale, -sub[i]);
+                        p0 = __builtin_amdgcn_exp2f(x0);
+                    }
+                    if (end) {
+                        const float p1 = __builtin_amdgcn_exp2f(x1);
+                        total[i] += p0;
+                        total[i] += p1;
+                        high[i] = fmaxf(fmaxf(now[i][v], now[i][v + 1]), high[i]);
+                        w.put(i, v, p0, p1);
+                    }
+                };
+                // (sums and maxima stay in their slot, too: left to itself the compiler collects them behind the body)
+                auto close = [&]() {
 #pragma unroll
                     for (int i = 0; i < QT; ++i) asm volatile("" : "+v"(total[i]), "+v"(high[i]));
                     __builtin_amdgcn_sched_barrier(0);
+                };
+                if constexpr (FIRST) fetch(LEAD / BT);
+#pragma unroll
+                for (int n = FIRST ? LEAD : 0; n < GROUPS; ++n) {
+                    const int b = n / BT, k = n % BT;
+                    const bool keys = n >= LEAD && n < LEAD + KS;
+                    const bf16x8 x = op[b == 0 ? 2 : b & 1][k];
+                    const int o = n < LEAD ? n : n - KS;
+                    const int e0 = FIRST ? (n - LEAD) * SHARE1 : n * SHARE, pairs = (FIRST ? SHARE1 : SHARE) / 2;
+#pragma unroll
+                    for (int i = 0; i < QT; ++i) {
+                        if (keys) next[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][keys ? n - LEAD : 0], next[i], 0, 0, 0);
+                        else if (!FIRST) acc[i][keys ? 0 : o % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, before.at(i, keys ? 0 : o / DB), acc[i][keys ? 0 : o % DB], 0, 0, 0);
+                        if (i == 0 && k == 0) fetch(b + 1);
+                        if (QT == 1) {
+#pragma unroll
+                            for (int z = 0; z < pairs; ++z) weigh(e0 + 2 * z, true, true);
+                        } else if (pairs == 1) weigh(e0, i == 0, i == 1);
+                        else {
+#pragma unroll
+                            for (int z = i * pairs / 2; z < (i + 1) * pairs / 2; ++z) weigh(e0 + 2 * z, true, true);
+                        }
+                        close();
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < QT; ++i) asm volatile("" : "+v"(next[i]));     // (scores where the vector instructions read them)
                 prev = slot;
                 slot = after;
                 ++s;
