@@ -130,7 +130,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
     using V = Row<T>;
     constexpr int E = sizeof(T), EPV = V::kPerVec;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    float2* turns = reinterpret_cast<float2*>(lds);                 // [tile][TS]
+    // A token's factors, TS apart, two dimensions' in 16 bytes: bfloat16 the vectors' first such pieces, then the second ones ..., so that
+    // neighbouring lanes read neighbouring pieces (dense 8192 tokens, 40 heads of 128: 44.5 -> 39.3 us; a vector's four pieces together
+    // were half conflicts); float32 a vector's two together (the gradient of 4099 tokens 11.0 us, apart 12.0).
+    constexpr int PIECES = EPV / 2;
+    float2* turns = reinterpret_cast<float2*>(lds);
     __shared__ int s_slot[kRotaryTokens], s_run[kRotaryTokens], s_runs;
     const int tid = threadIdx.x, D = A.D, n = A.n, half = n / 2;
     const int DP = (D + EPV - 1) / EPV * EPV, TS = DP + 2;            // (rows of factors start in different banks)
@@ -149,20 +153,34 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
         const int s = A.slots[t0 + tid];
         s_slot[tid] = s >= 0 && s < A.slot_count ? s : -1;
     }
+    const int vecs = DP / EPV;
+    auto piece_at = [&](int v, int piece) { return PIECES == 4 ? piece * vecs + v : v * PIECES + piece; };
     if (h0 < turned) {
+        // (the last vector of a row ends with it: where rows are no whole vectors it overlaps the one before)
+        auto put = [&](int t, int d, float c, float s) {
+            float2* row = turns + t * TS;
+            const float2 f = {c, s};
+            if (D == DP) {
+                row[PIECES == 4 ? ((d & 7) / 2 * vecs + d / 8) * 2 + (d & 1) : d] = f;
+                return;
+            }
+            const int v = d / EPV, e = d - v * EPV, last = d - (D - EPV);
+            if (v < vecs - 1) row[piece_at(v, e / 2) * 2 + (e & 1)] = f;
+            if (last >= 0) row[piece_at(vecs - 1, last / 2) * 2 + (last & 1)] = f;
+        };
         for (int i = tid; i < tokens * half; i += 256) {
             const int t = i / half, p = i - t * half;
             float c, s;
             turn_of((double)A.positions[t0 + t] * A.sign * A.inv_freq[p], c, s);
             c = (float)(c * A.magnitude);
             s = (float)(s * A.magnitude);
-            turns[t * TS + (INTERLEAVED ? 2 * p : p)] = {c, -s};
-            turns[t * TS + (INTERLEAVED ? 2 * p + 1 : p + half)] = {c, s};
+            put(t, INTERLEAVED ? 2 * p : p, c, -s);
+            put(t, INTERLEAVED ? 2 * p + 1 : p + half, c, s);
         }
-        const int rest = DP - n;
+        const int rest = D - n;
         for (int i = tid; i < tokens * rest; i += 256) {
             const int t = i / rest;
-            turns[t * TS + n + (i - t * rest)] = {1.f, -0.f};
+            put(t, n + (i - t * rest), 1.f, -0.f);
         }
     }
     __syncthreads();
@@ -180,7 +198,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
             if constexpr (ACROSS) v.more = load16_any(row);
         }
     };
-    auto turn = [&](const Vec& v, int t, int d0, float (&f)[EPV]) {
+    auto turn = [&](const Vec& v, int t, int vec, int d0, float (&f)[EPV]) {
         float x[EPV], y[EPV];
         V::unpack(v.own, x);
         if constexpr (INTERLEAVED) {
@@ -205,9 +223,13 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
                 }
             }
         }
-        const float2* w = turns + t * TS + d0;
+        const f32x4* w = reinterpret_cast<const f32x4*>(turns + t * TS);
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) f[e] = fmaf(x[e], w[e].x, (d0 + e < n ? y[e] : 0.f) * w[e].y);
+        for (int e = 0; e < EPV; e += 2) {
+            const f32x4 z = w[piece_at(vec, e / 2)];
+            f[e] = fmaf(x[e], z[0], (d0 + e < n ? y[e] : 0.f) * z[1]);
+            f[e + 1] = fmaf(x[e + 1], z[2], (d0 + e + 1 < n ? y[e + 1] : 0.f) * z[3]);
+        }
     };
     auto k_place = [&](int head, int slot, int d0) {               // of a key's vector in the cache
         const int page = slot / A.page, off = slot - page * A.page;
@@ -215,12 +237,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
         return reinterpret_cast<u32x4*>((char*)A.k_cache + (atom + (d0 * 2 + off % kAtom) * 8) * 2);
     };
     constexpr int BATCH = 4;                                        // vectors whose loads are under way at once
-    const int vecs = DP / EPV;
     const bool across = cached && stage != 0;                       // keys go to the cache token by token, neighbours in neighbouring lanes
     const int hb = min(h1, across ? A.q_heads : turned), hc = hb - h0;
     // (the last vector of a row ends with it; what it shares with the one before is the same twice)
     auto start_of = [&](int v) { return min(v * EPV, D - EPV); };
-    const int rows = 256 / vecs, row0 = tid / vecs, d0 = start_of(tid - row0 * vecs);
+    const int rows = 256 / vecs, row0 = tid / vecs, vec = tid - row0 * vecs, d0 = start_of(vec);
     if (hc > 0 && row0 < rows) {
         const int dt = rows / hc, dh = rows - dt * hc;
         int t = row0 / hc, h = row0 - t * hc;
@@ -243,7 +264,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
                 float f[EPV];
-                turn(v[u], tok[u], d0, f);
+                turn(v[u], tok[u], vec, d0, f);
                 const bool isq = at[u] < A.q_heads;
                 const int token = t0 + tok[u], head = isq ? at[u] : at[u] - A.q_heads;
                 const u32x4 r = V::pack(f);
@@ -278,7 +299,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
 #pragma unroll
                 for (int u = 0; u < BATCH; ++u) {
                     float f[EPV];
-                    turn(v[u], t, from[u], f);
+                    turn(v[u], t, from[u] / EPV, from[u], f);
                     if (i + 16 * u < count) *k_place(head[u], slot, from[u]) = V::pack(f);
                 }
             }
