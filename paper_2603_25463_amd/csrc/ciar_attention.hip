@@ -811,7 +811,7 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
                             // (both halves of the product's rows are this atom's tokens: the first eight accumulators are what is wanted)
 #pragma unroll 1
                             for (int k = 0; k < KS; ++k) {
-                                bf16x8 kk = *reinterpret_cast<const bf16x8*>(keys + (kread & (ATOM - 1)) + k * 512), qq = q[i][0];
+                                bf16x8 kk = *reinterpret_cast<const bf16x8*>(keys + kread - (col >> 4) * ATOM + k * 512), qq = q[i][0];
 #pragma unroll
                                 for (int z = 1; z < KS; ++z)
                                     if (k == z) qq = q[i][z];

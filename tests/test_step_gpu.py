@@ -378,7 +378,9 @@ def test_attention_of_strided_rows(ciar):
 
 
 @pytest.mark.parametrize("reqs,Hq,Hk,D", [([(100, 20)], 4, 2, 64), ([(70, 8), (40, 40)], 8, 1, 128), ([(300, 150)], 2, 2, 128),
-                                          ([(1500, 4)], 8, 2, 128), ([(90, 40)], 2, 1, 256)])
+                                          ([(1500, 4)], 8, 2, 128), ([(90, 40)], 2, 1, 256), ([(300, 200)], 4, 2, 96),
+                                          ([(2000, 300)], 2, 1, 96), ([(700, 260)], 2, 1, 192), ([(100, 3), (90, 70)], 2, 2, 160),
+                                          ([(1000, 400)], 1, 1, 224), ([(2500, 500)], 4, 1, 64)])
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
 def test_attention_keeps_what_a_row_does_not_see_out_of_it(ciar, reqs, Hq, Hk, D, bad):
     """The last new token's key and value are not finite: rows before it are as if they were not there."""
