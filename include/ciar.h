@@ -396,7 +396,8 @@ int ciar_interhead_logits_timed(const void* hidden, const void* weight, const fl
  *   slots, positions, requests [T]   cache slot (-1: not granted, or no token), position in the request (0: no token) and
  *                                    request (-1: no token) of each new token
  * Preconditions: 0 <= lengths, kept, new_tokens; 0 <= held <= table_width; no page twice in the ring and the tables.  What
- * breaks them gives unspecified numbers, never a fault.  table_width * page_size and ring_pages * page_size <= 2^31 - 1.
+ * breaks them gives unspecified numbers, never a fault.  table_width * page_size and ring_pages * page_size <= 2^31 - 1; R and T
+ * <= 2^30 - 1.
  */
 int ciar_cache_plan(const int32_t* lengths, const int32_t* kept, const int32_t* new_tokens, const int32_t* held, int64_t R,
                     int32_t* ring, int64_t ring_pages, const int64_t* ring_state, int32_t* table, int32_t table_width,
@@ -428,7 +429,7 @@ typedef struct ciar_rotary_params {
  *   q_out [T, q_heads, D]                  out     k_out [T, kv_heads, D]  out, without a cache
  * With a cache (k_cache, v_cache, slots and v [T, kv_heads, D] all given, k_out NULL) the turned keys and the values go to
  * slots [T] int32 of the cache instead; a slot outside the cache is left out (-1: a token without a place), and no slot may come twice.
- * Outputs must not overlap inputs.  Any alignment of q, k, v and their outputs; caches 16-byte aligned.
+ * Outputs must not overlap inputs.  Any alignment of q, k, v and their outputs; caches 16-byte aligned.  T <= 2^30 - 1.
  */
 int ciar_rotary(const void* q, const void* k, const void* v, const int32_t* positions, const double* inv_freq, int64_t T,
                 const ciar_rotary_params* params, void* q_out, void* k_out, void* k_cache, void* v_cache,

@@ -76,7 +76,7 @@ int ciar_cache_plan(const int32_t* lengths, const int32_t* kept, const int32_t* 
                     int32_t* positions, int32_t* requests, void* hip_stream)
 {
     if (R < 0 || T < 0) return fail(CIAR_EINVAL, "R or T is negative");
-    if (R > kMost || T >= kMost) return fail(CIAR_EUNSUPPORTED, "R or T exceeds 2^31 - 2");
+    if (R > kMost / 2 || T > kMost / 2) return fail(CIAR_EUNSUPPORTED, "R or T exceeds 2^30 - 1");
     if (int rc = check_pages(page_size, ring_pages, "ring_pages")) return rc;
     if (table_width < 1) return fail(CIAR_EINVAL, "table_width must be >= 1 (got %d)", table_width);
     if (table_width > kMost / page_size) return fail(CIAR_EUNSUPPORTED, "table_width * page_size exceeds 2^31 - 1 positions");
@@ -129,10 +129,10 @@ int ciar_rotary(const void* q, const void* k, const void* v, const int32_t* posi
     if (p->head_dim > 1024) return fail(CIAR_EUNSUPPORTED, "head_dim %d is above 1024", p->head_dim);
     if (!std::isfinite(p->magnitude)) return fail(CIAR_EINVAL, "params->magnitude is not finite");
     if (T < 0) return fail(CIAR_EINVAL, "T is negative");
-    if (T > kMost) return fail(CIAR_EUNSUPPORTED, "T exceeds 2^31 - 1");
+    if (T > kMost / 2) return fail(CIAR_EUNSUPPORTED, "T exceeds 2^30 - 1");
     const bool cached = k_cache || v_cache || slots;
     if (cached) {
-        if (!k_cache || !v_cache || !slots) return fail(CIAR_EINVAL, "k_cache, v_cache and slots go together");
+        if (!k_cache || !v_cache || (T > 0 && !slots)) return fail(CIAR_EINVAL, "k_cache, v_cache and slots go together");
         if (k_out) return fail(CIAR_EINVAL, "k_out is not written where a cache is given");
         if (p->dtype != CIAR_BF16) return fail(CIAR_EUNSUPPORTED, "the cache holds bfloat16: params->dtype must be CIAR_BF16");
         if (p->head_dim % 8 != 0) return fail(CIAR_EUNSUPPORTED, "head_dim %d is not a multiple of 8, as the cache needs", p->head_dim);
@@ -291,6 +291,7 @@ int ciar_adjust_logits(const void* logits, int64_t N, const ciar_params* params,
     const int elt = params->dtype == CIAR_F32 ? 4 : 2;
     if (out_stride < params->vocab) return fail(CIAR_EINVAL, "out_stride is smaller than vocab %d", params->vocab);
     if (out_stride * elt % 16 != 0) return fail(CIAR_EALIGN, "out_stride is not a multiple of 16 bytes");
+    if (N == 0) return CIAR_OK;                                    // (empty lists have no address)
     if ((j->history_start != nullptr) != (j->history != nullptr) || (j->prompt_len && !j->history_start))
         return fail(CIAR_EINVAL, "history_start and history go together, and prompt_len needs them");
     if ((j->bias_start != nullptr) != (j->bias_ids != nullptr) || (j->bias_ids != nullptr) != (j->bias_values != nullptr))
@@ -300,7 +301,6 @@ int ciar_adjust_logits(const void* logits, int64_t N, const ciar_params* params,
     if (j->allowed && (j->mask_rows < 1 || j->allowed_stride < (params->vocab + 31) / 32))
         return fail(CIAR_EINVAL, "allowed needs a row and %d words a row (mask_rows %d, allowed_stride %lld)",
                     (params->vocab + 31) / 32, j->mask_rows, (long long)j->allowed_stride);
-    if (N == 0) return CIAR_OK;
     if (!logits || !out) return fail(CIAR_EINVAL, "logits or out is NULL");
     if (!aligned(logits, 16) || !aligned(out, 16)) return fail(CIAR_EALIGN, "logits or out is not 16-byte aligned");
     const int64_t V = params->vocab, W = (N + params->window - 1) / params->window;

@@ -420,6 +420,27 @@ def test_attention_takes_pages_outside_the_cache_without_harm(ciar):
     check_attention({k: v[:7] for k, v in o.items()}, q[:7], [kv[0], (kv[1][0][:0], kv[1][1][:0])], [3, 4], [0, 3], 1 / math.sqrt(D), 2)
 
 
+def test_calls_without_tokens(ciar):
+    """Nothing to do: no launch, no complaint about lists that have no address."""
+    kc, vc, table, _ = make_cache(ciar, [4], 2, 64, 16, seed=1)
+    none = torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    o = ciar.rotary(none, none, i32([]), freqs(64), v=none, k_cache=kc, v_cache=vc, slots=i32([]))
+    assert o["q"].shape == (0, 2, 64)
+    assert ciar.rotary(none, none, i32([]), freqs(64))["k"].shape == (0, 2, 64)
+    o = ciar.paged_attention(none, kc, vc, table, i32([0, 0]), i32([4]), 0, 4)
+    assert o["out"].shape == (0, 2, 64) and o["lse"].shape == (0, 2)
+    e = torch.empty(0, device="cuda")
+    o = ciar.adjust_logits(torch.empty((0, 40), device="cuda"), ciar.Params(window=4), history_start=torch.zeros(1, dtype=torch.int64, device="cuda"),
+                           history=i32([]), drafted=i32([]), repetition=e, allowed=torch.zeros((1, 2), dtype=torch.int32, device="cuda"),
+                           allowed_row=i32([]))
+    assert o["logits"].shape == (0, 40) and o["left"].numel() == 0
+    x = torch.randn((3, 40), device="cuda")
+    zeros = torch.zeros(2, dtype=torch.int64, device="cuda")
+    o = ciar.adjust_logits(x, ciar.Params(window=4), history_start=zeros, history=i32([]), prompt_len=i32([0]), bias_start=zeros, bias_ids=i32([]),
+                           bias_values=e)
+    assert torch.equal(o["logits"], x)
+
+
 def test_attention_without_requests(ciar):
     kc, vc, table, _ = make_cache(ciar, [4], 1, 64, 16, seed=1)
     q = torch.randn((3, 2, 64)).bfloat16().cuda()

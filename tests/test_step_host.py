@@ -199,3 +199,11 @@ def test_binding_refuses_what_the_kernels_do_not_read():
         ciar.rotary(q, q, i32(3), f)                                             # not on the GPU
     with pytest.raises(ValueError):
         ciar.adjust_logits(torch.zeros((2, 8)), ciar.Params())
+
+
+def test_counts_at_their_limits(L):
+    """Counts above 2^30 - 1 are refused, and empty lists need no address."""
+    assert _plan(L, R=1 << 30) == EUNSUP and _plan(L, T=1 << 30) == EUNSUP
+    assert _rotary(L, T=1 << 30) == EUNSUP
+    assert _rotary(L, T=0, q=None, k=None, v=None, positions=None, slots=None, q_out=None) == 0
+    assert _adjust(L, N=0, history=None, drafted=None, bias_ids=None, bias_values=None) == 0
