@@ -151,8 +151,9 @@ constexpr float kSlack = 32.f;
 // themselves, each with all the rows and a softmax of its own; keys and values go from memory into the registers that the matrix
 // instructions take them from (the cache is laid out for that), requested a step ahead, through no LDS and past no barrier: what
 // bounds this kernel is memory.  At the end the waves' rows meet in LDS.  Keys and values are read once in a call and pass the caches
-// by (non-temporal): one token of 64 requests over 4096 149 -> 140 us, windows over 4100 58.4 -> 54.6, one token over 200001 46.7 -> 42.7
-// (inputs that change from call to call; the same 200 MB again and again come from the memory-side cache, 32 us against 50).
+// by (non-temporal): one token of 64 requests over up to 4096 149 -> 140 us (816 MB: 5.8 TB/s), windows of 8 tokens, 64 rows, of 32 requests over
+// up to 4100 58.4 -> 53.5 (208 MB), one token over 200001 46.7 -> 44.1 (205 MB; inputs that change from call to call; the same 200 MB again
+// and again come from the memory-side cache, 32 us against 50).
 //
 // Scores as S^T = K Q^T: a lane's accumulators belong to one row (l % 16), so that reference and sum stay in the lane.  Two products
 // of 16 tokens make a step, their tokens chosen so that a lane's eight weights are eight consecutive tokens, as the second product
@@ -452,6 +453,8 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
 // bits 2 and 3 of the token swapped, which makes a lane's accumulators consecutive tokens): they are the second product's operand
 // as they are.  A wave has its SIMD to itself, so its vector instructions have to run while its own matrix instructions do:
 // the loop's body computes the weights of step s next to the scores of step s + 1 and the output of step s - 1, all independent.
+// Chunks of three prompts of up to 2048 tokens behind up to 8192, 32 heads on 8 of 128: 518 us, 963 TFLOP/s (a large library product on the
+// card: 1200 to 1240); matrix instructions are at work in 49 % of the busy cycles, vector instructions issue in 47 %.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 using lds_ptr = __attribute__((address_space(3))) void*;
 using mem_ptr = const __attribute__((address_space(1))) void*;
@@ -958,7 +961,7 @@ constexpr int kJoinFew = 8;                                        // parts that
 // A kind of shape and what it takes, in us, with what the kernels measured.  Workgroups run in rounds of as many as the compute units
 // hold; a part costs its steps, a start and an end, and parts cost the launch that joins them, and the writing and reading of their
 // rows.  Few rows: 0.65 us a step of four waves at 128 dimensions while memory keeps up (5.5 TB/s over all) and 6 to 12 us a workgroup (64
-// rows); many rows: 3.4 TFLOP/s a unit and 15 us; joining: 6 us and 4 TB/s.  (Windows of 8 tokens, 32 requests, 128 units of 64 rows over 4100
+// rows); many rows: 3.4 TFLOP/s a unit (short calls; 3.8 in long ones) and 15 us; joining: 6 us and 4 TB/s.  (Windows of 8 tokens, 32 requests, 128 units of 64 rows over 4100
 // tokens: 1 part 69 us, 2 parts 54.6; one token, 2 units over 200001: 64 parts 56.6 us, 128 parts 42.7; one token, 512 units over
 // 4096: 1 part 140 us, 2 parts 149.)
 double cost_of(const AttentionArgs& a, bool many, int rows_each, Shape* s)

