@@ -447,6 +447,8 @@ typedef struct ciar_attention_params {
     int32_t  reserved;        /* must be 0                                                                  */
     int64_t  table_stride, cache_pages;
     int64_t  q_stride, q_head_stride, out_stride, out_head_stride;
+    int64_t  total_len;       /* all requests together have no more tokens in the cache; 0: not known.  Only how the work is
+                                 divided depends on it: worth giving where contexts differ a lot */
 } ciar_attention_params;
 
 /* Bytes of device workspace ciar_paged_attention needs for R requests and T new tokens (0: none). */
@@ -463,6 +465,7 @@ size_t ciar_attention_workspace_bytes(int64_t R, int64_t T, const ciar_attention
  * effect on it.
  *   q [T, q_heads, D] bf16  in      table [R, table_width] int32, cu_new [R + 1], kv_len [R] int32  in
  *   out [T, q_heads, D] bf16, lse [T, q_heads] float  out (lse may be NULL)
+ * max_new, max_len and total_len are promises: rows that break them get unspecified numbers.
  * table entries are clamped into the cache, kv_len into [0, min(max_len, table_width * page_size)] and cu_new into [0, T].
  */
 int ciar_paged_attention(const void* q, const void* k_cache, const void* v_cache, const int32_t* table,

@@ -120,6 +120,35 @@ struct Unit {
     int r, h, block, split;            // request, key head, block of rows, part of the tokens
 };
 
+constexpr int kSteps = 32;             // tokens of a step: two atoms
+
+// Steps of a part of a unit of `steps`: as many as make `splits` parts of any unit, or `part` in all of them.
+__device__ __forceinline__ int part_of(int steps, int splits, int part) { return part > 0 ? part : (steps + splits - 1) / splits; }
+
+// Where contexts differ, all parts are of the same length, a long context's are many, and the grid holds what total_len says there can be: the
+// units' requests and parts are found from the lengths, 64 requests at a time.  (One token for a context of 100000 and 63 of 1000, 8 key heads of
+// 128: one part for each 1220 us, 24 parts 121; with places in the grid for 24 parts of every context 313, 2.3 ns for each place with
+// nothing in it, and many parts on one XCD.  32 contexts of 200 to 50000, windows of 8: 328 -> 165.)
+__device__ __forceinline__ bool ragged_unit(const AttentionArgs& A, int place, int part, int& r, int& split)
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int r0 = 0; r0 < A.R; r0 += 64) {
+        const int len = r0 + lane < A.R ? min(max(A.kv_len[r0 + lane], 0), A.max_len) : 0;
+        const int mine = r0 + lane < A.R ? max(((len + kSteps - 1) / kSteps + part - 1) / part, 1) : 0;
+        const int upto = before + (int)wave_scan((double)mine);
+        const unsigned long long after = __ballot(upto > place);
+        if (after) {
+            const int l = __ffsll((long long)after) - 1;
+            r = r0 + l;
+            split = place - __builtin_amdgcn_readlane(upto - mine, l);
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
 // Which page an atom of a request lies in: atom / (page / 16) for any page size, as a multiplication (2 atom < 2^32; the
 // multiplier is 2^(31 + shift) / (page / 16) rounded up, with 2^shift >= page / 16, which is exact for every atom below 2^31).
 struct Pages {
@@ -134,8 +163,6 @@ Pages pages_of(int page)
     p.mul = (uint32_t)(((1ull << (31 + p.shift)) + p.per - 1) / p.per);
     return p;
 }
-
-constexpr int kSteps = 32;             // tokens of a step: two atoms
 
 // The reference of a softmax (its weights are 2^(s - reference)) stands still: it is the largest score of the first step that a wave takes,
 // which most rows' later scores do not exceed by much, and weights of up to 2^kSlack lose nothing in 32 bits or bfloat16.  The largest score
@@ -159,7 +186,7 @@ constexpr float kSlack = 32.f;
 // of 16 tokens make a step, their tokens chosen so that a lane's eight weights are eight consecutive tokens, as the second product
 // (O^T = V^T P^T) wants them: the first takes tokens 8 g .. 8 g + 3 of the step as its rows 4 g ..., the second 8 g + 4 ....
 template <int D, int RT>
-__global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, const Pages P, int blocks, int splits, int64_t work,
+__global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, const Pages P, int blocks, int splits, int part, int64_t work,
                                                        float* __restrict__ part_o, float2* __restrict__ part_s)
 {
     constexpr int ROWF = D + 4;                                    // floats of a row in LDS
@@ -173,10 +200,16 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
     Unit u;
     {
         int i = blockIdx.x;
-        u.split = i % splits; i /= splits;
-        u.block = i % blocks; i /= blocks;
-        u.h = i % A.kv_heads;
-        u.r = i / A.kv_heads;
+        if (__builtin_expect(part > 0, 0)) {
+            u.h = i % A.kv_heads; i /= A.kv_heads;
+            u.block = i % blocks;
+            if (!ragged_unit(A, i / blocks, part, u.r, u.split)) return;
+        } else {
+            u.split = i % splits; i /= splits;
+            u.block = i % blocks; i /= blocks;
+            u.h = i % A.kv_heads;
+            u.r = i / A.kv_heads;
+        }
     }
     const int g = A.q_heads / A.kv_heads;
     const Request R = request_of(A, u.r);
@@ -184,7 +217,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const AttentionArgs A, co
     if (m0 >= rows) return;
     const int most = min(max(R.base + min(m0 + 16 * RT - 1, rows - 1) / g + 1, 0), R.len);        // what the last row sees
     const int least = min(max(R.base + m0 / g + 1, 0), R.len);                                    // and the first
-    const int steps = (most + kSteps - 1) / kSteps, each = (steps + splits - 1) / splits;
+    const int steps = (most + kSteps - 1) / kSteps, each = part_of(steps, splits, part);
     const int first = u.split * each, last = min(first + each, steps);
     if (first >= last && u.split > 0) return;                      // (a row that sees nothing is the first part's)
 
@@ -480,7 +513,7 @@ struct Weights {
 };
 
 template <int D, int QT>
-__global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A, const Pages P, int blocks, int splits, int64_t work,
+__global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A, const Pages P, int blocks, int splits, int part, int64_t work,
                                                            float* __restrict__ part_o, float2* __restrict__ part_s)
 {
     constexpr int KS = D / 16, DB = D / 32;                        // slices of 16 dimensions, blocks of 32
@@ -497,9 +530,14 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
     {
         int i = blockIdx.x;
         u.h = i % A.kv_heads; i /= A.kv_heads;
-        u.split = i % splits; i /= splits;
-        u.block = blocks - 1 - i % blocks;                         // the blocks that see most come first
-        u.r = i / blocks;
+        if (__builtin_expect(part > 0, 0)) {
+            u.block = blocks - 1 - i % blocks;
+            if (!ragged_unit(A, i / blocks, part, u.r, u.split)) return;
+        } else {
+            u.split = i % splits; i /= splits;
+            u.block = blocks - 1 - i % blocks;                     // the blocks that see most come first
+            u.r = i / blocks;
+        }
     }
     const int g = A.q_heads / A.kv_heads;
     const Request R = request_of(A, u.r);
@@ -508,7 +546,7 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
     if (m0 >= rows) return;
     const int most = min(max(R.base + min(m0 + ROWS - 1, rows - 1) / g + 1, 0), R.len);
     const int least = min(max(R.base + m0 / g + 1, 0), R.len);
-    const int steps = (most + kSteps - 1) / kSteps, each = (steps + splits - 1) / splits;
+    const int steps = (most + kSteps - 1) / kSteps, each = part_of(steps, splits, part);
     const int first = u.split * each, last = min(first + each, steps);
     if (first >= last && u.split > 0) return;
     const int full = min(max(least / kSteps, first), last);        // steps that every row sees whole: [first, full)
@@ -888,7 +926,7 @@ __global__ __launch_bounds__(256, 1) void many_rows_kernel(const AttentionArgs A
 // exchange, with many (WIDE) a workgroup takes one row and its groups deal the parts among themselves.  Two rounds of loads: sums and
 // references of the group's parts, then their outputs.
 template <int D, bool WIDE>
-__global__ __launch_bounds__(256) void join_kernel(const AttentionArgs A, int blocks, int rows_per_block, int splits,
+__global__ __launch_bounds__(256) void join_kernel(const AttentionArgs A, int blocks, int rows_per_block, int splits, int part,
                                                    const float* __restrict__ part_o, const float2* __restrict__ part_s)
 {
     constexpr int TPR = D / 4, GROUPS = 256 / TPR, ROWS = WIDE ? 1 : GROUPS;
@@ -907,7 +945,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttentionArgs A, int bl
     if (!WIDE && !mine) return;
     if (WIDE && m >= rows) return;                                 // (the whole workgroup)
     const int most = min(max(R.base + min(m0 + rows_per_block - 1, rows - 1) / g + 1, 0), R.len);
-    const int steps = (most + kSteps - 1) / kSteps, each = (steps + splits - 1) / splits;
+    const int steps = (most + kSteps - 1) / kSteps, each = part_of(steps, splits, part);
     const int parts = each > 0 ? (steps + each - 1) / each : 1;    // those that have written
     const int j = m / g, head = h * g + (m - j * g);
     const int64_t t = R.begin + j, at = t * A.q_heads + head, step = (int64_t)A.T * A.q_heads;
@@ -954,7 +992,8 @@ __global__ __launch_bounds__(256) void join_kernel(const AttentionArgs A, int bl
 // How a call is laid out: rows of a workgroup, blocks of rows per request and key head, parts of the tokens.
 struct Shape {
     bool many;
-    int rows, blocks, splits;
+    int rows, blocks, splits, part;                                // (`part`: steps of one, 0: a unit's share)
+    int64_t work;                                                  // workgroups
 };
 constexpr int kJoinFew = 8;                                        // parts that join_kernel takes one after another
 
@@ -976,15 +1015,35 @@ double cost_of(const AttentionArgs& a, bool many, int rows_each, Shape* s)
     const int64_t resident = (int64_t)compute_units() * per_unit;
     const double step_us = many ? 4.0 * kSteps * rows_each * a.D / 3.4e6 : 0.65 * a.D / 128, wg_us = many ? 15.0 : rows_each == 64 ? 12.0 : 6.0;
     const int64_t steps = ((int64_t)a.max_len + kSteps - 1) / kSteps;
-    const double memory_us = many ? 0.0 : (double)units * steps * (4 * kSteps * a.D) / 5.5e6;
     const double row_us = (double)a.T * a.q_heads * (a.D * 8 + 16) / 4e6;
+    // Steps of all units: as many as if every context were the longest, or what total_len leaves (a context's last step is one of its own).
+    const int64_t at_most = units * steps, told = a.total_len > 0 ? (a.total_len / kSteps + a.R) * a.kv_heads * s->blocks : at_most;
+    const int64_t all = told < at_most ? told : at_most;
     s->splits = 1;
+    s->part = 0;
     double best = 0.0;
+    const double memory_us = many ? 0.0 : (double)all * (4 * kSteps * a.D) / 5.5e6;
     for (int64_t n = 1; n <= 256 && n <= (steps + 3) / 4; n += n < 16 ? 1 : n < 64 ? 4 : 16) {
-        const int64_t rounds = (units * n + resident - 1) / resident, each = (steps + n - 1) / n;
-        const double own = (double)rounds * ((double)each * step_us + wg_us), least = memory_us + wg_us;
-        const double us = (own > least ? own : least) + (n > 1 ? 6.0 + (double)n * row_us : 0.0);
-        if (n == 1 || us < 0.95 * best) { best = us; s->splits = (int)n; }
+        const int64_t each = (steps + n - 1) / n;
+        double own, times = (double)n;                             // parts of a row
+        if (all == at_most) {
+            own = (double)((units * n + resident - 1) / resident) * ((double)each * step_us + wg_us);
+        } else {
+            // contexts that differ: the parts there are, dealt as units become free, and the last of them
+            const int64_t parts = n == 1 ? units : all / each + units < units * n ? all / each + units : units * n;
+            const double dealt = ((double)all * step_us + (double)parts * wg_us) / (double)resident, alone = (double)each * step_us + wg_us;
+            times = (double)parts / (double)units;
+            own = (dealt > alone ? dealt : alone);
+        }
+        const double least = memory_us + wg_us;
+        const double us = (own > least ? own : least) + (n > 1 ? 6.0 + times * row_us : 0.0);
+        if (n == 1 || us < 0.95 * best) { best = us; s->splits = (int)n; s->part = n > 1 && all < at_most ? (int)each : 0; }
+    }
+    s->work = units * s->splits;
+    if (s->part > 0) {
+        // (a context's last part is one of its own)
+        const int64_t places = (a.total_len / ((int64_t)kSteps * s->part) + a.R) * a.kv_heads * s->blocks;
+        if (places < s->work) s->work = places;
     }
     return best;
 }
@@ -1026,14 +1085,14 @@ hipError_t launch_many(const AttentionArgs& a, const Shape& s, unsigned grid, in
             raised[dev].store(true, std::memory_order_release);
         }
     }
-    hipLaunchKernelGGL((many_rows_kernel<D, QT>), dim3(grid), dim3(256), bytes, stream, a, pages_of(a.page), s.blocks, s.splits, work, po, ps);
+    hipLaunchKernelGGL((many_rows_kernel<D, QT>), dim3(grid), dim3(256), bytes, stream, a, pages_of(a.page), s.blocks, s.splits, s.part, work, po, ps);
     return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_shape(const AttentionArgs& a, const Shape& s, void* workspace, hipStream_t stream)
 {
-    const int64_t work = (int64_t)a.R * a.kv_heads * s.blocks * s.splits, grid = work + 32;
+    const int64_t work = s.work, grid = work + 32;
     constexpr int at_once = 256 / (D / 4);                         // rows of a workgroup of join_kernel
     const bool wide = s.splits > kJoinFew;
     const int64_t join = (int64_t)a.R * a.kv_heads * s.blocks * (wide ? s.rows : (s.rows + at_once - 1) / at_once);
@@ -1048,15 +1107,15 @@ hipError_t launch_shape(const AttentionArgs& a, const Shape& s, void* workspace,
         else e = launch_many<D, 1>(a, s, (unsigned)grid, work, po, ps, stream);
     } else {
         const Pages P = pages_of(a.page);
-        if (s.rows == 16) hipLaunchKernelGGL((few_rows_kernel<D, 1>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
+        if (s.rows == 16) hipLaunchKernelGGL((few_rows_kernel<D, 1>), g, b, 0, stream, a, P, s.blocks, s.splits, s.part, work, po, ps);
         else if constexpr (D > 192) return hipErrorInvalidValue;
-        else if (s.rows == 32) hipLaunchKernelGGL((few_rows_kernel<D, 2>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
-        else if constexpr (D <= 128) hipLaunchKernelGGL((few_rows_kernel<D, 4>), g, b, 0, stream, a, P, s.blocks, s.splits, work, po, ps);
+        else if (s.rows == 32) hipLaunchKernelGGL((few_rows_kernel<D, 2>), g, b, 0, stream, a, P, s.blocks, s.splits, s.part, work, po, ps);
+        else if constexpr (D <= 128) hipLaunchKernelGGL((few_rows_kernel<D, 4>), g, b, 0, stream, a, P, s.blocks, s.splits, s.part, work, po, ps);
         e = hipGetLastError();
     }
     if (e != hipSuccess || s.splits == 1) return e;
-    if (wide) hipLaunchKernelGGL((join_kernel<D, true>), dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, po, ps);
-    else hipLaunchKernelGGL((join_kernel<D, false>), dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, po, ps);
+    if (wide) hipLaunchKernelGGL((join_kernel<D, true>), dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, s.part, po, ps);
+    else hipLaunchKernelGGL((join_kernel<D, false>), dim3((unsigned)join), b, 0, stream, a, s.blocks, s.rows, s.splits, s.part, po, ps);
     return hipGetLastError();
 }
 

@@ -206,7 +206,7 @@ int attention_args(int64_t R, int64_t T, const ciar_attention_params* p, ciar::A
     if (int rc = check_pages(p->page_size, p->cache_pages, "cache_pages")) return rc;
     if (p->table_width < 1) return fail(CIAR_EINVAL, "table_width must be >= 1 (got %d)", p->table_width);
     if (p->table_width > kMost / p->page_size) return fail(CIAR_EUNSUPPORTED, "table_width * page_size exceeds 2^31 - 1 positions");
-    if (p->max_new < 0 || p->max_len < 0) return fail(CIAR_EINVAL, "max_new or max_len is negative");
+    if (p->max_new < 0 || p->max_len < 0 || p->total_len < 0) return fail(CIAR_EINVAL, "max_new, max_len or total_len is negative");
     if (!std::isfinite(p->scale)) return fail(CIAR_EINVAL, "params->scale is not finite");
     if (R < 0 || T < 0) return fail(CIAR_EINVAL, "R or T is negative");
     if (R > 65535) return fail(CIAR_EUNSUPPORTED, "R exceeds 65535 requests per call");
@@ -216,6 +216,7 @@ int attention_args(int64_t R, int64_t T, const ciar_attention_params* p, ciar::A
     std::memset(a, 0, sizeof *a);
     a->scale = p->scale;
     a->table_stride = p->table_stride;
+    a->total_len = p->total_len < (int64_t)kMost * 65536 ? p->total_len : (int64_t)kMost * 65536;
     a->R = (int32_t)R; a->T = (int32_t)T; a->q_heads = p->q_heads; a->kv_heads = p->kv_heads; a->D = p->head_dim;
     a->page = p->page_size; a->pages = (int32_t)p->cache_pages; a->width = p->table_width;
     // no request has more rows than there are, nor more tokens than its row of pages holds

@@ -46,7 +46,7 @@ struct AttentionArgs {
     const void *   k_cache, *v_cache;
     const int32_t *table, *cu_new, *kv_len;
     float*         lse;                                // may be null
-    int64_t        table_stride;
+    int64_t        table_stride, total_len;            // total_len: most tokens of all requests, 0: not known
     float          scale;
     int32_t        R, T, q_heads, kv_heads, D, page, pages, width, max_new, max_len;
 };

@@ -404,12 +404,12 @@ PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* k
     });
 }
 
-enum { A_Q, A_KC, A_VC, A_TABLE, A_CU, A_LEN, A_MAXNEW, A_MAXLEN, A_SCALE, A_STREAM, A_OUT, A_WORKSPACE, A_COUNT };
+enum { A_Q, A_KC, A_VC, A_TABLE, A_CU, A_LEN, A_MAXNEW, A_MAXLEN, A_SCALE, A_TOTAL, A_STREAM, A_OUT, A_WORKSPACE, A_COUNT };
 PyObject* attention_names[A_COUNT];
 PyObject *s_out, *s_lse;
 
 // The sizes of an attention call.
-ciar_attention_params attention_params(const at::Tensor& q, const Cache& c, const at::Tensor& table, PyObject* max_new, PyObject* max_len)
+ciar_attention_params attention_params(const at::Tensor& q, const Cache& c, const at::Tensor& table, PyObject* max_new, PyObject* max_len, PyObject* total_len)
 {
     if (q.dim() != 3) value_error("q must be [T, heads, D]");
     if (q.size(1) > INT32_MAX || table.size(1) > INT32_MAX) value_error("q or table is too large");
@@ -422,6 +422,7 @@ ciar_attention_params attention_params(const at::Tensor& q, const Cache& c, cons
     p.table_width = (int32_t)table.size(1);
     p.max_new = integer32(max_new, "max_new");
     p.max_len = integer32(max_len, "max_len");
+    p.total_len = total_len && total_len != Py_None ? integer(total_len, "total_len") : 0;
     p.table_stride = row_stride(table);
     p.cache_pages = c.pages;
     p.scale = (float)(1.0 / std::sqrt((double)c.dim));
@@ -436,7 +437,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs, Py
         const at::Tensor &q = tensor(a.v[A_Q], "q"), &table = tensor(a.v[A_TABLE], "table");
         const Cache c = cache(a.v[A_KC], a.v[A_VC]);
         const auto* tp = (const int32_t*)matrix(table, "table");
-        ciar_attention_params p = attention_params(q, c, table, a.v[A_MAXNEW], a.v[A_MAXLEN]);
+        ciar_attention_params p = attention_params(q, c, table, a.v[A_MAXNEW], a.v[A_MAXLEN], a.v[A_TOTAL]);
         if (a.given(A_SCALE)) p.scale = (float)number(a.v[A_SCALE], "scale");
         const int64_t T = q.size(0), Hq = q.size(1), R = table.size(0);
         const void* qp = head_rows(q, "q", at::kBFloat16, T, Hq, c.dim);
@@ -465,7 +466,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs, Py
     });
 }
 
-enum { W_Q, W_KC, W_TABLE, W_MAXNEW, W_MAXLEN, W_COUNT };
+enum { W_Q, W_KC, W_TABLE, W_MAXNEW, W_MAXLEN, W_TOTAL, W_COUNT };
 PyObject* attention_bytes_names[W_COUNT];
 
 PyObject* attention_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
@@ -476,7 +477,7 @@ PyObject* attention_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t
         const at::Tensor &q = tensor(a.v[W_Q], "q"), &k = tensor(a.v[W_KC], "k_cache"), &table = tensor(a.v[W_TABLE], "table");
         if (k.dim() != 6 || table.dim() != 2) value_error("k_cache or table has the wrong number of dimensions");
         const Cache c = {nullptr, nullptr, k.size(0), k.size(1), k.size(2) * 16, k.size(3) * 8};
-        const ciar_attention_params p = attention_params(q, c, table, a.v[W_MAXNEW], a.v[W_MAXLEN]);
+        const ciar_attention_params p = attention_params(q, c, table, a.v[W_MAXNEW], a.v[W_MAXLEN], a.v[W_TOTAL]);
         return PyLong_FromSize_t(ciar_attention_workspace_bytes(table.size(0), q.size(0), &p));
     });
 }
@@ -574,13 +575,14 @@ PyMethodDef methods[] = {
      "of the turned tensors' gradients it makes those of q and k.  With ``v``, ``k_cache``, ``v_cache`` and ``slots`` int32 [T]\n"
      "(bfloat16) the turned keys and the values go into the cache.  Returns q, and k without a cache; ``out`` may carry them."},
     {"paged_attention", CIAR_FAST(paged_attention),
-     "paged_attention(q, k_cache, v_cache, table, cu_new, kv_len, max_new, max_len, *, scale=None, stream=None, out=None, workspace=None) -> dict\n--\n\n"
+     "paged_attention(q, k_cache, v_cache, table, cu_new, kv_len, max_new, max_len, *, scale=None, total_len=None, stream=None, out=None, workspace=None) -> dict\n--\n\n"
      "``ciar_paged_attention``: the new tokens ``q`` [T, heads, D] (bfloat16) of R requests over the cache.  ``table`` int32\n"
      "[R, width], ``cu_new`` int32 [R + 1], ``kv_len`` int32 [R]; no request has more than ``max_new`` new tokens and\n"
-     "``max_len`` tokens in the cache.  ``scale`` defaults to 1 / sqrt(D).  Returns out [T, heads, D] bfloat16 and lse\n"
+     "``max_len`` tokens in the cache.  ``scale`` defaults to 1 / sqrt(D).  ``total_len``, which all requests'\n"
+     "tokens together do not exceed, helps to divide the work where contexts differ a lot.  Returns out [T, heads, D] bfloat16 and lse\n"
      "[T, heads] float32; ``out`` may carry them."},
     {"attention_workspace_bytes", CIAR_FAST(attention_workspace_bytes),
-     "attention_workspace_bytes(q, k_cache, table, max_new, max_len) -> int\n--\n\nBytes of workspace ``paged_attention`` asks for (0: none)."},
+     "attention_workspace_bytes(q, k_cache, table, max_new, max_len, total_len=None) -> int\n--\n\nBytes of workspace ``paged_attention`` asks for (0: none)."},
     {"adjust_logits", CIAR_FAST(adjust_logits),
      "adjust_logits(logits, params, *, history_start=None, history=None, prompt_len=None, drafted=None, repetition=None, presence=None, frequency=None, "
      "bias_start=None, bias_ids=None, bias_values=None, allowed=None, allowed_row=None, vocab=None, stream=None, out=None, workspace=None) -> dict\n--\n\n"
@@ -608,8 +610,8 @@ PyMODINIT_FUNC PyInit__step()
     if (!intern(plan_names, {"lengths", "new", "held", "ring", "ring_state", "table", "tokens", "page_size", "kept", "stream", "out"}) ||
         !intern(plan_outputs, {"lengths", "kv_len", "cu_new", "held", "granted", "ring_state", "slots", "positions", "requests"}) ||
         !intern(rotary_names, {"q", "k", "positions", "inv_freq", "layout", "inverse", "magnitude", "v", "k_cache", "v_cache", "slots", "stream", "out"}) ||
-        !intern(attention_names, {"q", "k_cache", "v_cache", "table", "cu_new", "kv_len", "max_new", "max_len", "scale", "stream", "out", "workspace"}) ||
-        !intern(attention_bytes_names, {"q", "k_cache", "table", "max_new", "max_len"}) ||
+        !intern(attention_names, {"q", "k_cache", "v_cache", "table", "cu_new", "kv_len", "max_new", "max_len", "scale", "total_len", "stream", "out", "workspace"}) ||
+        !intern(attention_bytes_names, {"q", "k_cache", "table", "max_new", "max_len", "total_len"}) ||
         !intern(adjust_names, {"logits", "params", "history_start", "history", "prompt_len", "drafted", "repetition", "presence", "frequency",
                                "bias_start", "bias_ids", "bias_values", "allowed", "allowed_row", "vocab", "stream", "out", "workspace"}) ||
         !intern(&s_window, {"window"}) || !intern(&s_cuda_stream, {"cuda_stream"}) || !intern(&s_half, {"half"}) ||

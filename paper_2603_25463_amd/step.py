@@ -39,7 +39,7 @@ class _AttentionParams(ctypes.Structure):
         "q_heads", "kv_heads", "head_dim", "page_size", "table_width", "max_new", "max_len")] + [
         ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
         (n, ctypes.c_int64) for n in ("table_stride", "cache_pages", "q_stride", "q_head_stride", "out_stride",
-                                      "out_head_stride")]
+                                      "out_head_stride", "total_len")]
 
 
 class _Adjustments(ctypes.Structure):

@@ -420,6 +420,37 @@ def test_attention_takes_pages_outside_the_cache_without_harm(ciar):
     check_attention({k: v[:7] for k, v in o.items()}, q[:7], [kv[0], (kv[1][0][:0], kv[1][1][:0])], [3, 4], [0, 3], 1 / math.sqrt(D), 2)
 
 
+TOLD = {  # [(tokens in the cache, new)], q heads, kv heads, D, page
+    "one_long": ([(20, 1)] * 5 + [(9000, 1)] + [(33, 1)] * 6, 8, 2, 64, 16),
+    "beyond_64": ([(7, 1)] * 70 + [(6000, 1)] + [(40, 1)] * 75 + [(3000, 1)], 4, 1, 64, 16),
+    "windows": ([(5000, 8), (100, 8), (64, 7), (0, 3), (33, 8), (8, 8)], 8, 1, 128, 32),
+    "wide_parts": ([(14000, 2), (1, 1), (17, 2), (0, 0)], 4, 4, 128, 16),
+    "chunks": ([(3500, 90), (100, 100), (90, 17), (64, 1)], 8, 1, 128, 64), "chunks_192": ([(40, 30), (2500, 140)], 4, 2, 192, 16),
+    "d256": ([(4000, 1), (30, 2), (0, 2)], 2, 1, 256, 48),
+}
+
+
+@pytest.mark.parametrize("name", list(TOLD))
+def test_attention_of_contexts_that_differ(ciar, name):
+    """Told how many tokens there are in all, the work is divided by the lengths on the GPU: every row is held to the formula."""
+    reqs, Hq, Hk, D, page = TOLD[name]
+    lens, news = [a for a, _ in reqs], [b for _, b in reqs]
+    say("[attention told]", name, len(reqs))
+    kc, vc, table, kv = make_cache(ciar, lens, Hk, D, page, seed=3 + len(name))
+    T = sum(news)
+    starts = [sum(news[:i]) for i in range(len(news))]
+    q = torch.randn((T, Hq, D), generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    cu, kl = i32(starts + [T]), i32(lens)
+    scale = 1 / math.sqrt(D)
+    for total in (sum(lens), sum(lens) + 500):
+        args = (q, kc, vc, table, cu, kl, max(news), max(lens))
+        assert ciar.attention_workspace_bytes(q, kc, table, max(news), max(lens), total) > 0      # (so that parts are what is tested)
+        o = ciar.paged_attention(*args, total_len=total)
+        check_attention(o, q, kv, news, starts, scale, Hq // Hk)
+        p = ciar.paged_attention(*args, total_len=total)
+        assert torch.equal(o["out"], p["out"]) and torch.equal(o["lse"], p["lse"])
+
+
 def test_calls_without_tokens(ciar):
     """Nothing to do: no launch, no complaint about lists that have no address."""
     kc, vc, table, _ = make_cache(ciar, [4], 2, 64, 16, seed=1)

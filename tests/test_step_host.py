@@ -207,3 +207,14 @@ def test_counts_at_their_limits(L):
     assert _rotary(L, T=1 << 30) == EUNSUP
     assert _rotary(L, T=0, q=None, k=None, v=None, positions=None, slots=None, q_out=None) == 0
     assert _adjust(L, N=0, history=None, drafted=None, bias_ids=None, bias_values=None) == 0
+
+
+def test_attention_told_of_all_tokens(L):
+    """total_len only says how to divide the work: one long context among short ones gets parts, equal contexts are as without it."""
+    from paper_2603_25463_amd.step import _AttentionParams
+    def need(total, R=64, longest=100000, rows=1):
+        c = _AttentionParams(ctypes.sizeof(_AttentionParams), 32, 8, 128, 16, 1 << 20, rows, longest, 0.1, 0, 1 << 20, 1 << 20, 4096, 128,
+                             4096, 128, total)
+        return L.ciar_attention_workspace_bytes(R, R * rows, ctypes.byref(c))
+    assert need(100000 + 63 * 1000) > 0 and need(0) == need(64 * 100000) == need(1 << 62)
+    assert _attention(L, struct=dict(total_len=-1)) == EINVAL
