@@ -40,6 +40,13 @@ __device__ __forceinline__ u32x4 load16_any(const void* p)
     return v;
 }
 
+// The same past the caches, where no other thread wants them.  Of a row's way in and its way out one goes past the caches: in, where pairs
+// lie side by side (a vector is read once), out, where a partner's vector is read by its own thread, too; keys and values of the cache always.
+// (8192 tokens, 48 heads of 128 into a cache, side by side: neither way 51.4 us, both 49.2, this 46.0; halves 53.5, this 49.7;
+// 40 heads without a cache 39.4 -> 34.7 and 39.3 -> 36.6.)
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ u32x4 load16_once(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4_any*>(p)); }
+
 template <typename T> struct Row;
 template <> struct Row<float> {
     static constexpr int kPerVec = 4;
@@ -124,7 +131,7 @@ __global__ __launch_bounds__(256) void rotary_short_kernel(const RotaryArgs A)
 // wants a dimension's eight tokens side by side.  Tiles begin where an atom of the cache begins if the tokens' slots are
 // consecutive (the first token's slot says where): a dimension's eight tokens are then one store; runs that are cut off are stored
 // element by element.  Bound by memory: 16 bytes in, 16 out, four multiply-adds to an 8-byte pair.  8192 tokens of 48 heads of 128 into a
-// cache, half of a head turned: 51 us, 3.9 TB/s (a large copy 4.7); 4099 tokens of 20 heads of 80 in float32 11.2 us.
+// cache, half of a head turned: 46 us, 4.4 TB/s (a large copy 4.7); 4099 tokens of 20 heads of 80 in float32 11 us.
 template <typename T, bool INTERLEAVED, bool ACROSS>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int tile, int heads_per_wg, int stage)
 {
@@ -132,7 +139,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
     constexpr int E = sizeof(T), EPV = V::kPerVec;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     // A token's factors, TS apart, two dimensions' in 16 bytes: bfloat16 the vectors' first such pieces, then the second ones ..., so that
-    // neighbouring lanes read neighbouring pieces (dense 8192 tokens, 40 heads of 128: 44.5 -> 39.3 us; a vector's four pieces together
+    // neighbouring lanes read neighbouring pieces (dense 8192 tokens, 40 heads of 128: 44.5 -> 39.3 us then; a vector's four pieces together
     // were half conflicts); float32 a vector's two together (the gradient of 4099 tokens 11.0 us, apart 12.0).
     constexpr int PIECES = EPV / 2;
     float2* turns = reinterpret_cast<float2*>(lds);
@@ -190,7 +197,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
         u32x4 own, other, more;
     };
     auto load = [&](Vec& v, const char* row, int d0) {
-        v.own = load16_any(row + d0 * E);
+        v.own = INTERLEAVED ? load16_once(row + d0 * E) : load16_any(row + d0 * E);
         if constexpr (!INTERLEAVED) {
             // partners: the vector half a turn further or back; across the middle of the pairs the last of the second half and the first
             // of the first; dimensions that are only copied fetch themselves
@@ -273,7 +280,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
                 if (isq || !cached) {
                     char* p = (char*)(isq ? A.q_out.p : A.k_out.p);
                     const int64_t ts = isq ? A.q_out.token : A.k_out.token, hs = isq ? A.q_out.head : A.k_out.head;
-                    __builtin_memcpy(p + (token * ts + head * hs + d0) * E, &r, 16);
+                    u32x4_any* to = reinterpret_cast<u32x4_any*>(p + (token * ts + head * hs + d0) * E);
+                    if constexpr (INTERLEAVED) *to = r;
+                    else __builtin_nontemporal_store(r, to);
                 } else if (E == 2) {
                     const int slot = s_slot[tok[u]];
                     if (slot >= 0) *k_place(head, slot, d0) = r;
@@ -301,7 +310,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
                 for (int u = 0; u < BATCH; ++u) {
                     float f[EPV];
                     turn(v[u], t, from[u] / EPV, from[u], f);
-                    if (i + 16 * u < count) *k_place(head[u], slot, from[u]) = V::pack(f);
+                    if (i + 16 * u < count) __builtin_nontemporal_store(V::pack(f), k_place(head[u], slot, from[u]));
                 }
             }
     }
@@ -343,7 +352,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
                 const int j = min(i + 256 * u, nh * tokens * per - 1), row = j / per, t = row / nh, h = row - t * nh;
-                r[u] = load16_any(static_cast<const char*>(A.v.p) + ((t0 + t) * A.v.token + (hv + h - turned) * A.v.head + (j - row * per) * 8) * 2);
+                r[u] = load16_once(static_cast<const char*>(A.v.p) + ((t0 + t) * A.v.token + (hv + h - turned) * A.v.head + (j - row * per) * 8) * 2);
             }
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
@@ -368,7 +377,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs A, int til
                     u32x4 r;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) r[e] = from[2 * e * RS] | (uint32_t)from[(2 * e + 1) * RS] << 16;
-                    *reinterpret_cast<u32x4*>(to) = r;
+                    __builtin_nontemporal_store(r, reinterpret_cast<u32x4*>(to));
                 } else
                     for (int e = 0; e < len; ++e) to[e] = from[e * RS];
             }
