@@ -243,6 +243,85 @@ def test_rotary_into_the_cache(ciar, T, Hq, Hk, D, n, page, start, layout, order
     assert bool((rows_k[rest] == 9.0).all()) and bool((rows_v[rest] == -9.0).all())
 
 
+@pytest.mark.parametrize("T,Hq,Hk,D,n,page", [(1024, 2, 1, 128, 128, 16), (1500, 1, 3, 96, 34, 32), (3001, 4, 2, 64, 64, 48), (1203, 1, 1, 256, 200, 64),
+                                              (1100, 3, 2, 264, 16, 16), (2000, 1, 1, 16, 16, 16), (1031, 2, 5, 40, 40, 32)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("order", ["chunk", "requests", "scattered"])
+def test_rotary_of_many_tokens_into_the_cache(ciar, T, Hq, Hk, D, n, page, layout, order):
+    """Sixteen tokens at a time: one long run of slots from an odd place, runs of one to forty tokens, every slot for itself; some have none."""
+    say("[rotary cache, many]", T, Hq, Hk, D, n, page, layout, order)
+    g = torch.Generator().manual_seed(T + D)
+    x = torch.randn((T, Hq + 2 * Hk, D), generator=g).bfloat16().cuda()
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hk], x[:, Hq + Hk:]
+    pages = (2 * T + 5) // page + 3
+    ks, vs = ciar.cache_shapes(pages, Hk, D, page)
+    kc, vc = torch.full(ks, 9.0).bfloat16().cuda(), torch.full(vs, -9.0).bfloat16().cuda()
+    own = torch.randperm(pages, generator=g)
+    i = torch.arange(T) + 5
+    if order == "requests":                                       # (a gap behind every run)
+        cut = torch.cumsum(torch.randint(1, 41, (T,), generator=g), 0)
+        i = i + torch.cumsum(torch.randint(0, 2, (T,), generator=g), 0)[torch.searchsorted(cut, torch.arange(T), right=True)]
+    slots = own[i // page] * page + i % page
+    if order == "scattered":
+        slots = slots[torch.randperm(T, generator=g)]
+    slots[torch.randint(0, T, (T // 50,), generator=g)] = -1
+    pos = torch.randint(0, 100000, (T,), generator=g, dtype=torch.int32).cuda()
+    f = freqs(n)
+    o = ciar.rotary(q, k, pos, f, layout=layout, v=v, k_cache=kc, v_cache=vc, slots=slots.int().cuda())
+    torch.cuda.synchronize()
+    want, size = rotary_reference(q, pos, f, layout, 1.0, False)
+    check_rotary(o["q"], want, size, torch.bfloat16)
+    rows_k = kc.permute(0, 2, 4, 1, 3, 5).reshape(pages * page, Hk, D).cpu()
+    rows_v = vc.permute(0, 2, 3, 5, 1, 4).reshape(pages * page, Hk, D).cpu()
+    ok = slots >= 0
+    want, size = rotary_reference(k, pos, f, layout, 1.0, False)
+    check_rotary(rows_k[slots[ok]], want[ok], size[ok], torch.bfloat16)
+    assert torch.equal(rows_v[slots[ok]], v.cpu()[ok])
+    rest = torch.ones(pages * page, dtype=torch.bool)
+    rest[slots[ok]] = False
+    assert bool((rows_k[rest] == 9.0).all()) and bool((rows_v[rest] == -9.0).all())
+
+
+@pytest.mark.parametrize("new,tokens", [(3, 100), (150, 400)])
+def test_offsets_beyond_32_bits(ciar, new, tokens):
+    """Caches of 5 GB each, used at their far end, and rows of q and out 2^31 elements apart."""
+    Hq, Hk, D, page = 4, 8, 128, 64
+    pages = 40000
+    ks, vs = ciar.cache_shapes(pages, Hk, D, page)
+    kc, vc = (torch.empty(s, dtype=torch.bfloat16, device="cuda") for s in (ks, vs))
+    assert kc.numel() > 1 << 31
+    g = torch.Generator().manual_seed(new)
+    need = -(-tokens // page)
+    own = pages - 1 - torch.randperm(need, generator=g)
+    i = torch.arange(tokens)
+    slots = (own[i // page] * page + i % page).int().cuda()
+    k, v = (torch.randn((tokens, Hk, D), generator=g).bfloat16() for _ in range(2))
+    still = torch.zeros(tokens, dtype=torch.int32, device="cuda")
+    ciar.rotary(torch.zeros((tokens, 1, D)).bfloat16().cuda(), k.cuda(), still, freqs(D), v=v.cuda(), k_cache=kc, v_cache=vc, slots=slots)
+    apart = (1 << 31) // new + 8
+    qs, ys = (torch.empty(apart * (new - 1) + 2 * Hq * D, dtype=torch.bfloat16, device="cuda").as_strided((new, Hq * 2, D), (apart, D, 1)) for _ in range(2))
+    assert apart * (new - 1) * 2 > 1 << 31
+    x = torch.randn((new, 2 * Hq, D), generator=g).bfloat16()
+    qs.copy_(x)
+    table = own.int()[None].cuda()
+    o = ciar.paged_attention(qs, kc, vc, table, i32([0, new]), i32([tokens]), new, tokens, out={"out": ys})
+    check_attention({"out": ys, "lse": o["lse"]}, x, [(k.double(), v.double())], [new], [0], 1 / math.sqrt(D), 1)
+    turned = ciar.rotary(qs, qs, still[:new], freqs(D), out={"q": ys})
+    assert torch.equal(turned["k"].cpu(), x) and torch.equal(ys.cpu(), x)
+
+
+def test_logit_rows_beyond_32_bits(ciar):
+    V, apart = 5000, (1 << 31) + 64
+    rows = torch.empty(2 * apart + V, dtype=torch.bfloat16, device="cuda").as_strided((3, V), (apart, 1))
+    x = torch.randn((3, V), generator=torch.Generator().manual_seed(2)).bfloat16()
+    rows.copy_(x)
+    words = torch.full((1, -(-V // 32)), 0x55555555, dtype=torch.int32, device="cuda")
+    o = ciar.adjust_logits(rows, ciar.Params(window=3), allowed=words, allowed_row=i32([0, -1, 0]), out={"logits": rows})
+    want = x.clone()
+    want[0, 1::2] = want[2, 1::2] = -math.inf
+    assert torch.equal(rows.cpu(), want) and o["left"].tolist() == [V // 2, V, V // 2]
+
+
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 def test_rotary_gradient(ciar, layout):
     """The inverse turn is the gradient: against autograd of the formula in 64 bits, and against differences."""
