@@ -826,3 +826,69 @@ def test_attention_of_scores_that_climb(ciar, step, new, D):
     o = ciar.paged_attention(q.cuda(), kc, vc, table, i32([0, new]), i32([L]), new, L, scale=1.0)
     assert bool(torch.isfinite(o["out"].float()).all())
     check_attention(o, q, kv, [new], [0], 1.0, Hq // Hk)
+
+
+MANY_ROWS = [  # D, [(tokens in the cache, new)], q heads, kv heads, page: what the matrix cores' kernel takes, 128 and 256 rows, whole and in parts
+    (32, [(600, 50), (599, 33), (310, 49), (64, 50)], 128, 64, 16), (32, [(130, 100), (129, 99), (100, 100), (128, 65)], 128, 32, 16),
+    (64, [(300, 33), (299, 32), (40, 33)], 128, 64, 32), (64, [(2000, 100), (1501, 99), (100, 100), (1999, 3)], 16, 16, 16),
+    (64, [(130, 130), (129, 100), (130, 77), (16, 16)], 64, 16, 16), (64, [(1500, 130), (1400, 130), (131, 129)], 32, 32, 16),
+    (96, [(130, 50), (129, 49), (50, 50)], 128, 64, 16), (96, [(2000, 33), (1999, 32), (33, 33), (700, 31)], 16, 8, 48),
+    (96, [(130, 130), (129, 129), (130, 1), (64, 64)], 32, 8, 16), (96, [(2000, 130), (1300, 130), (129, 65), (130, 130)], 8, 8, 16),
+    (128, [(130, 33), (129, 32), (64, 33)], 128, 64, 16), (128, [(2000, 33), (1999, 32), (33, 33), (700, 31)], 16, 8, 64),
+    (128, [(130, 130), (129, 129), (130, 5), (130, 64)], 32, 8, 32), (128, [(2000, 130), (1300, 130), (129, 65), (130, 130)], 8, 8, 16),
+    (160, [(130, 33), (129, 33), (40, 31)], 64, 32, 16), (160, [(1500, 33), (1499, 32), (33, 33)], 16, 16, 32),
+    (192, [(130, 33), (129, 33), (40, 31)], 64, 32, 16), (192, [(1000, 33), (999, 32), (33, 33), (512, 33)], 16, 16, 64),
+    (224, [(130, 33), (129, 33), (40, 31)], 32, 32, 16), (224, [(1000, 33), (999, 32), (33, 33), (512, 33)], 8, 8, 16),
+    (256, [(130, 33), (129, 33), (40, 31)], 32, 32, 48), (256, [(1000, 33), (999, 32), (33, 33), (512, 33)], 8, 8, 16),
+]
+
+
+FEW_ROWS = [  # the same, for the kernel of few rows: 16, 32 and 64 rows, in one part, a few, many
+    *((D, [(L, n)], h, 1, 16) for D in range(32, 257, 32) for h, n in ((3, 3), (4, 5)) for L in (40, 1000, 2000)),
+    (32, [(1000, 12), (999, 11), (33, 12)] * 6, 48, 16, 16), (64, [(1000, 24), (31, 20)] * 8, 24, 8, 16), (64, [(4000, 40), (3333, 39), (64, 1), (40, 40)], 8, 1, 64),
+    (96, [(40, 24), (39, 23)] * 8, 24, 8, 16), (96, [(4000, 12), (130, 12), (12, 9), (0, 3)] * 4, 6, 2, 48), (128, [(40, 24), (25, 24)] * 8, 24, 8, 16),
+    (128, [(2000, 40), (1025, 33)] * 8, 2, 2, 16), (128, [(4000, 40), (129, 40), (2222, 20), (40, 40)], 8, 1, 32),
+]
+
+
+def attention_case(ciar, case, kind, seed):
+    """plain; the first request's last key and value not finite, which only its last row sees; scores of the first request that climb out of
+    range; the tokens in all told."""
+    D, reqs, Hq, Hk, page = case
+    say("[attention]", kind, case)
+    lens, news = [a for a, _ in reqs], [b for _, b in reqs]
+    kc, vc, table, kv = make_cache(ciar, lens, Hk, D, page, seed=seed)
+    starts, T, L = [sum(news[:i]) for i in range(len(news))], sum(news), lens[0]
+    i = torch.arange(L)
+    pages, atom, t = table[0].cpu()[i // page].long().cuda(), (i % page // 16).cuda(), (i % 16).cuda()
+    q = torch.randn((T, Hq, D), generator=torch.Generator().manual_seed(seed)).bfloat16()
+    if kind in ("inf", "nan"):
+        kc[pages[-1], :, atom[-1], :, t[-1]] = vc[pages[-1], :, atom[-1], t[-1] // 8, :, t[-1] % 8] = float(kind)
+    if kind == "climb":
+        q[:news[0]] = 1.0 / D
+        kv[0][0][:] = (3.0 * (i // 8)).bfloat16().double()[:, None, None]
+        kv[0][1][:] = torch.where(i % 2 == 0, -2e33, 1e33).bfloat16().double()[:, None, None]
+        kc[pages, :, atom, :, t] = kv[0][0].bfloat16().cuda().view(L, Hk, D // 8, 8)
+        vc[pages, :, atom, t // 8, :, t % 8] = kv[0][1].bfloat16().cuda()
+    scale = 1.0 if kind == "climb" else 1 / math.sqrt(D)
+    o = ciar.paged_attention(q.cuda(), kc, vc, table, i32(starts + [T]), i32(lens), max(news), max(lens), scale=scale,
+                             total_len=sum(lens) if kind == "told" else None)
+    torch.cuda.synchronize()
+    if kind in ("inf", "nan"):
+        n = news[0] - 1
+        assert bool(torch.isnan(o["out"][n]).any())
+        o, q = {k: torch.cat([v[:n], v[n + 1:]]) for k, v in o.items()}, torch.cat([q[:n], q[n + 1:]])
+        kv, news, starts = [(kv[0][0][:-1], kv[0][1][:-1])] + kv[1:], [n] + news[1:], [0] + [b - 1 for b in starts[1:]]
+    check_attention(o, q, kv, news, starts, scale, Hq // Hk)
+
+
+@pytest.mark.parametrize("case", range(len(MANY_ROWS)))
+@pytest.mark.parametrize("kind", ["plain", "inf", "nan", "climb", "told"])
+def test_attention_of_many_rows(ciar, case, kind):
+    attention_case(ciar, MANY_ROWS[case], kind, case)
+
+
+@pytest.mark.parametrize("case", range(len(FEW_ROWS)))
+@pytest.mark.parametrize("kind", ["plain", "nan", "climb", "told"])
+def test_attention_of_few_rows(ciar, case, kind):
+    attention_case(ciar, FEW_ROWS[case], kind, case)
