@@ -43,7 +43,7 @@ __device__ __forceinline__ u32x4 load16_any(const void* p)
 // The same past the caches, where no other thread wants them.  Of a row's way in and its way out one goes past the caches: in, where pairs
 // lie side by side (a vector is read once), out, where a partner's vector is read by its own thread, too; keys and values of the cache always.
 // (8192 tokens, 48 heads of 128 into a cache, side by side: neither way 51.4 us, both 49.2, this 46.0; halves 53.5, this 49.7;
-// 40 heads without a cache 39.4 -> 34.7 and 39.3 -> 36.6.)
+// 40 heads without a cache 39.4 -> 34.7 and 39.3 -> 36.6; behind a kernel that has just written the rows 51.7 -> 41.4 and 53.5 -> 42.7.)
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ u32x4 load16_once(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4_any*>(p)); }
 
